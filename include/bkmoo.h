@@ -447,6 +447,165 @@ bkmoo_status bkmoo_set_resolve_path(int32_t path);
  */
 bkmoo_status bkmoo_set_wait_limit(uint32_t polls);
 
+/* ------------------------------------------------------------------------
+ * A layer's training step around the resolve.  The backward passes below write
+ * each task's weight gradients where bkmoo_resolve reads them: into that task's
+ * row of the gradient buffer.  A batch holds its tasks' rows one after another
+ * (task k: rows task_rows[k] .. task_rows[k+1]), so that one pass over it
+ * gives all K tasks' gradients; bkmoo_adamw takes the resolved update.
+ *
+ * Shared conventions: matrices are row-major and contiguous, of one type `dt`;
+ * sums, statistics and activations are fp32, results rounded once to nearest
+ * even; non-finite values propagate.  Pointers need natural alignment (rows that
+ * start at 16 bytes take faster kernels); a workspace starts at 16 bytes and
+ * needs no initialisation.  task_rows (host) is int64[K+1] from 0 to M,
+ * non-decreasing, 1 <= K <= 16; a task without rows gets zero gradients.  Weight gradient k
+ * of a matrix starts task_stride elements after gradient k-1 (task_stride >=
+ * the matrix's elements if K > 1) and is written, not added to; it must not
+ * overlap the inputs or another gradient (not checked; other overlaps are
+ * BKMOO_EINVAL).  M = 0 is allowed.  Everything is queued on `stream`; nothing
+ * is allocated or synchronised.  Sums run in a fixed order: results are bitwise
+ * reproducible.
+ * ------------------------------------------------------------------------ */
+
+/* Activation of the gate. */
+typedef enum {
+  BKMOO_SILU = 0, /* u / (1 + exp(-u)) */
+  BKMOO_GELU = 1  /* tanh form: u/2 (1 + tanh(sqrt(2/pi) (u + 0.044715 u^3))) */
+} bkmoo_act;
+
+/* How bkmoo_adamw's moments are held. */
+typedef enum {
+  BKMOO_STATE_F32 = 0,
+  BKMOO_STATE_F8 = 1  /* e4m3 (finite, no infinities) times a scale per 256 elements */
+} bkmoo_state_dtype;
+
+/* One of bkmoo_adamw's tensors (host struct). */
+typedef struct {
+  void *data;    /* device, n elements */
+  int64_t n;     /* >= 0 */
+  int32_t decay; /* nonzero: weight decay applies */
+} bkmoo_tensor;
+
+/* Hyper-parameters of an AdamW step (host struct). */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* lr, wd >= 0; betas in [0, 1); eps > 0 (also in fp32) */
+  int64_t step;                               /* t >= 1: the first step is 1 */
+  uint32_t seed;                              /* random bits of BKMOO_STATE_F8: another for every step */
+} bkmoo_adamw_hparams;
+
+/*
+ * bkmoo_residual_norm_forward — the norm after a block, its gate and residual
+ * scale, and the norm before the next block, row by row (mean over the D
+ * elements of a row):
+ *
+ *   b  = scale * gate * (post_weight * y / sqrt(mean(y^2) + eps))
+ *   resid_out = resid + b
+ *   normed    = weight * r / sqrt(mean(r^2) + eps),  r = resid + b before rounding
+ *
+ *   resid, y               (in)  [M][D]
+ *   weight                 (in)  [D]
+ *   post_weight, gate      (in)  [D] or NULL: no norm after the block, no gate
+ *   resid_out, normed      (out) [M][D]; resid_out may be resid
+ *
+ * BKMOO_EUNSUPPORTED for rows of more than 64 KiB.
+ */
+bkmoo_status bkmoo_residual_norm_forward(int64_t M, int64_t D, bkmoo_dtype dt, const void *resid, const void *y,
+                                         const void *weight, const void *post_weight, const void *gate,
+                                         double scale, double eps, void *resid_out, void *normed,
+                                         hipStream_t stream);
+
+/* Workspace of bkmoo_residual_norm_backward (*bytes, host). */
+bkmoo_status bkmoo_residual_norm_workspace_size(int64_t M, int64_t D, int32_t K, size_t *bytes);
+
+/*
+ * bkmoo_residual_norm_backward — gradients of the above.
+ *
+ *   dresid_out             (in)  [M][D]: the loss's gradient by resid_out other than
+ *                                through normed, or NULL: zero
+ *   dnormed                (in)  [M][D]
+ *   resid_out, y           (in)  [M][D] as the forward pass left and got them; the
+ *                                statistics are made from them again
+ *   dresid, dy             (out) [M][D]; dresid may be dresid_out
+ *   dweight, dpost_weight, dgate (out) [K][D], task_stride apart, of dt; the last two exactly
+ *                                where post_weight and gate are given
+ */
+bkmoo_status bkmoo_residual_norm_backward(int64_t M, int64_t D, bkmoo_dtype dt, int32_t K, const int64_t *task_rows,
+                                          const void *dresid_out, const void *dnormed, const void *resid_out,
+                                          const void *y, const void *weight, const void *post_weight,
+                                          const void *gate, double scale, double eps, void *dresid, void *dy,
+                                          void *dweight, void *dpost_weight, void *dgate, int64_t task_stride,
+                                          void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Workspace of bkmoo_ffn_forward (backward 0) or bkmoo_ffn_backward (1) (*bytes, host). */
+bkmoo_status bkmoo_ffn_workspace_size(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, int32_t backward,
+                                      size_t *bytes);
+
+/*
+ * bkmoo_ffn_forward — gated feed-forward block:
+ *
+ *   u = x w_gate^T, v = x w_up^T, h = act(u) * v, y = h w_down^T
+ *
+ *   x [M][D]; w_gate, w_up [F][D]; w_down [D][F]   (in)
+ *   y [M][D]                                        (out)
+ *   gate_out, up_out [M][F]                         (out, both or neither NULL) u and v,
+ *                                                   for the backward pass
+ *
+ * For more than a few rows h is rounded to dt between the products.
+ * BKMOO_EUNSUPPORTED for D or F above 2^20.
+ */
+bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, bkmoo_act act, const void *x,
+                               const void *w_gate, const void *w_up, const void *w_down, void *y, void *gate_out,
+                               void *up_out, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * bkmoo_ffn_backward — gradients of the above, from dy and the products that
+ * the forward pass kept:
+ *
+ *   dh = dy w_down, du = dh v act'(u), dv = dh act(u), dx = du w_gate + dv w_up
+ *   task k, sums over its rows: dw_gate = du^T x, dw_up = dv^T x, dw_down = dy^T h
+ *
+ *   dx [M][D]; dw_gate, dw_up [K][F][D], dw_down [K][D][F], task_stride apart   (out)
+ *
+ * du, dv and h are rounded to dt between the products.
+ */
+bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, bkmoo_act act, int32_t K,
+                                const int64_t *task_rows, const void *dy, const void *x, const void *gate_out,
+                                const void *up_out, const void *w_gate, const void *w_up, const void *w_down,
+                                void *dx, void *dw_gate, void *dw_up, void *dw_down, int64_t task_stride,
+                                void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Blocks of 256 elements (the last of a tensor may be shorter) of T tensors (*blocks, host). */
+bkmoo_status bkmoo_adamw_blocks(int32_t T, const bkmoo_tensor *tensors, int64_t *blocks);
+
+/*
+ * bkmoo_adamw — one AdamW step over T tensors in one call:
+ *
+ *   g = grad_scale * grad, m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ *   tensors    (host array) the parameters, of type dt; the decay term applies where decay is set
+ *   grad       (in)  N = sum of n elements of grad_dt: the tensors' gradients one after another, as
+ *              bkmoo_resolve leaves them
+ *   moment1, moment2 (in/out) N elements in the same order.  BKMOO_STATE_F32: m and v, fp32.
+ *              BKMOO_STATE_F8: m and sqrt(v) as e4m3 times scales; zeros with zero scales to
+ *              start with
+ *   scales     (in/out, BKMOO_STATE_F8 alone) fp32 [2][blocks]: moment1's scales, then moment2's;
+ *              blocks from bkmoo_adamw_blocks
+ *   master     (in/out, may be NULL; dt bf16) fp32 [N]: takes the step; the tensors get its rounding
+ *   grad_scale (in, may be NULL: 1) device fp32: a clipping factor, say
+ *
+ * BKMOO_STATE_F8 rounds the moments stochastically, between the two e4m3 values around
+ * each, with 8 random bits a moment (16 if a beta is above 0.98) mixed from `seed` and
+ * the element's number; equal arguments give equal results.  A non-finite gradient makes its whole block's moments
+ * non-finite.  The hyper-parameters are taken when the call is made (a captured graph
+ * repeats them).
+ */
+bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmoo_dtype dt, int64_t N, const void *grad,
+                         bkmoo_dtype grad_dt, bkmoo_state_dtype state_dt, void *moment1, void *moment2,
+                         float *scales, int64_t blocks, float *master, const bkmoo_adamw_hparams *hp,
+                         const float *grad_scale, hipStream_t stream);
+
 /* Human-readable name of a status code (static string). */
 const char *bkmoo_status_string(bkmoo_status st);
 

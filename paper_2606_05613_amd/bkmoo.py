@@ -9,7 +9,8 @@ built, importing this module fails.
 Names mirror include/bkmoo.h: workspace_size, gram, solve, combine, resolve,
 resolve_noalloc, conflicts, slice_offsets, gram_reduce, resolve_path, resolve_traffic,
 read_device_error, set_resolve_path, set_wait_limit, set_grid_override,
-status_string.
+status_string; and for the layer around the resolve residual_norm_forward,
+residual_norm_backward, ffn_forward, ffn_backward, adamw_table, adamw.
 """
 
 from __future__ import annotations
@@ -28,6 +29,8 @@ METHODS = {"mgda": 0, "pcgrad": 1, "cagrad": 2, "mean": 3, "mgda-exact": 4, "cag
 DEVERR_OFFSETS = 0x1
 DEVERR_TIMEOUT = 0x2
 PATH_TWO_PASS, PATH_HYBRID, PATH_REFILL = 1, 3, 4
+ACTS = {"silu": 0, "gelu": 1}
+STATE_F32, STATE_F8 = 0, 1
 
 
 class BkmooError(RuntimeError):
@@ -39,12 +42,24 @@ class _Hparams(ctypes.Structure):
                 ("pcgrad_order", ctypes.c_void_p)]
 
 
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("decay", ctypes.c_int32)]
+
+
+class _AdamwHparams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64),
+                ("seed", ctypes.c_uint32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2606_05613_amd.build`")
     lib = ctypes.CDLL(LIB_PATH)
     i32, i64, sz, vp, u32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_uint32
     vpp = ctypes.POINTER(ctypes.c_void_p)
+    cint, f64 = ctypes.c_int, ctypes.c_double
+    i64p = ctypes.POINTER(i64)
     sig = {
         "bkmoo_workspace_size": [i32, i64, i32, ctypes.c_int, ctypes.POINTER(sz)],
         "bkmoo_gram": [i32, vpp, ctypes.c_int, i64, i32, vp, vp, vp, sz, vp],
@@ -65,6 +80,17 @@ def _load():
                                ctypes.POINTER(i32)],
         "bkmoo_set_resolve_path": [i32],
         "bkmoo_set_wait_limit": [u32],
+        "bkmoo_residual_norm_forward": [i64, i64, cint, vp, vp, vp, vp, vp, f64, f64, vp, vp, vp],
+        "bkmoo_residual_norm_workspace_size": [i64, i64, i32, ctypes.POINTER(sz)],
+        "bkmoo_residual_norm_backward": [i64, i64, cint, i32, i64p, vp, vp, vp, vp, vp, vp, vp, f64, f64,
+                                         vp, vp, vp, vp, vp, i64, vp, sz, vp],
+        "bkmoo_ffn_workspace_size": [i64, i64, i64, cint, i32, ctypes.POINTER(sz)],
+        "bkmoo_ffn_forward": [i64, i64, i64, cint, cint, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        "bkmoo_ffn_backward": [i64, i64, i64, cint, cint, i32, i64p, vp, vp, vp, vp, vp, vp, vp,
+                               vp, vp, vp, vp, i64, vp, sz, vp],
+        "bkmoo_adamw_blocks": [i32, ctypes.POINTER(_Tensor), i64p],
+        "bkmoo_adamw": [i32, ctypes.POINTER(_Tensor), cint, i64, vp, cint, cint, vp, vp, vp, i64, vp,
+                        ctypes.POINTER(_AdamwHparams), vp, vp],
         "bkmoo_status_string": [ctypes.c_int],
     }
     for name, args in sig.items():
@@ -80,7 +106,10 @@ EXPORTS = ("bkmoo_workspace_size", "bkmoo_gram", "bkmoo_solve", "bkmoo_combine",
            "bkmoo_resolve_noalloc",
            "bkmoo_conflicts", "bkmoo_slice_offsets", "bkmoo_gram_reduce", "bkmoo_resolve_traffic",
            "bkmoo_read_device_error", "bkmoo_set_grid_override", "bkmoo_resolve_path",
-           "bkmoo_set_resolve_path", "bkmoo_set_wait_limit", "bkmoo_status_string")
+           "bkmoo_set_resolve_path", "bkmoo_set_wait_limit",
+           "bkmoo_residual_norm_forward", "bkmoo_residual_norm_workspace_size", "bkmoo_residual_norm_backward",
+           "bkmoo_ffn_workspace_size", "bkmoo_ffn_forward", "bkmoo_ffn_backward", "bkmoo_adamw_blocks",
+           "bkmoo_adamw", "bkmoo_status_string")
 
 
 def status_string(st: int) -> str:
@@ -412,3 +441,233 @@ def set_resolve_path(path: int):
 
 def set_wait_limit(polls: int):
     _check(_lib.bkmoo_set_wait_limit(int(polls)), "bkmoo_set_wait_limit")
+
+
+# ----------------------------------------------------------------------------
+# the layer around the resolve
+# ----------------------------------------------------------------------------
+
+
+def _ptr(t: Optional[torch.Tensor], shape, like: torch.Tensor, what: str):
+    """Pointer of a contiguous tensor of `like`'s type and device; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != like.dtype or t.shape != shape or not t.is_contiguous() or t.device != like.device:
+        raise ValueError(f"{what} must be a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, what: str):
+    """Rows, columns and dtype code of a 2-D GPU tensor."""
+    code = _dt(t)
+    _gpu(t, what)
+    if t.dim() != 2:
+        raise ValueError(f"{what} must have two dimensions")
+    return t.shape[0], t.shape[1], code
+
+
+def _byte_workspace(ws: Optional[torch.Tensor], need: int, dev) -> torch.Tensor:
+    if ws is None:
+        return torch.empty(need, dtype=torch.uint8, device=dev)
+    if ws.dtype != torch.uint8 or ws.device != dev or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the inputs' device")
+    return ws
+
+
+def _task_rows(task_rows: Sequence[int], M: int):
+    rows = [0, M] if task_rows is None else [int(r) for r in task_rows]
+    if len(rows) < 2:
+        raise ValueError("task_rows holds K + 1 offsets from 0 to the number of rows")
+    return (ctypes.c_int64 * len(rows))(*rows), len(rows) - 1
+
+
+def _task_grads(grads, K: int, n: int, like: torch.Tensor):
+    """Pointers and the common distance of the tasks' gradients: [K, n] tensors whose rows
+    are contiguous (columns of the [K, N] gradient buffer), or None."""
+    stride, ptrs = None, []
+    for t, what in grads:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.dtype != like.dtype or t.shape != (K, n) or t.device != like.device or (n > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what} must be a {like.dtype} tensor of shape {(K, n)} with contiguous rows on "
+                             f"{like.device}")
+        if K > 1:
+            if stride is not None and t.stride(0) != stride:
+                raise ValueError("the tasks' gradients must be equally far apart in every tensor")
+            stride = t.stride(0)
+        ptrs.append(t.data_ptr())
+    return ptrs, n if stride is None else stride
+
+
+def residual_norm_forward(resid: torch.Tensor, y: torch.Tensor, weight: torch.Tensor,
+                          post_weight: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                          scale: float = 1.0, eps: float = 1e-6, resid_out: Optional[torch.Tensor] = None,
+                          normed: Optional[torch.Tensor] = None):
+    """The norm after a block (with post_weight), its gate and residual scale, and the
+    norm before the next: (resid + scale * gate * norm(y), norm of that), both [M, D].
+    resid_out may be resid."""
+    M, D, dt = _matrix(resid, "resid")
+    dev, shape, vec = resid.device, resid.shape, (D,)
+    if resid_out is None:
+        resid_out = torch.empty_like(resid, memory_format=torch.contiguous_format)
+    if normed is None:
+        normed = torch.empty_like(resid, memory_format=torch.contiguous_format)
+    args = (_ptr(resid, shape, resid, "resid"), _ptr(y, shape, resid, "y"), _ptr(weight, vec, resid, "weight"),
+            _ptr(post_weight, vec, resid, "post_weight"), _ptr(gate, vec, resid, "gate"), scale, eps,
+            _ptr(resid_out, shape, resid, "resid_out"), _ptr(normed, shape, resid, "normed"))
+    with torch.cuda.device(dev):
+        _check(_lib.bkmoo_residual_norm_forward(M, D, dt, *args, _stream_ptr(dev)), "bkmoo_residual_norm_forward")
+    return resid_out, normed
+
+
+def residual_norm_backward(dresid_out: Optional[torch.Tensor], dnormed: torch.Tensor, resid_out: torch.Tensor,
+                           y: torch.Tensor, weight: torch.Tensor, post_weight: Optional[torch.Tensor] = None,
+                           gate: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-6,
+                           task_rows: Optional[Sequence[int]] = None, dweight: Optional[torch.Tensor] = None,
+                           dpost_weight: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                           dresid: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None):
+    """Gradients of residual_norm_forward: returns (dresid, dy) and writes the K tasks'
+    weight gradients to dweight, dpost_weight and dgate, [K, D] with contiguous rows
+    (columns of the gradient buffer).  task_rows: K + 1 offsets of the tasks' rows."""
+    M, D, dt = _matrix(resid_out, "resid_out")
+    dev, shape, vec, like = resid_out.device, resid_out.shape, (D,), resid_out
+    rows, K = _task_rows(task_rows, M)
+    if dweight is None:
+        raise ValueError("dweight is needed")
+    ptrs, stride = _task_grads(((dweight, "dweight"), (dpost_weight, "dpost_weight"), (dgate, "dgate")), K, D, like)
+    if dresid is None:
+        dresid = torch.empty_like(resid_out, memory_format=torch.contiguous_format)
+    if dy is None:
+        dy = torch.empty_like(resid_out, memory_format=torch.contiguous_format)
+    need = ctypes.c_size_t(0)
+    _check(_lib.bkmoo_residual_norm_workspace_size(M, D, K, ctypes.byref(need)), "bkmoo_residual_norm_workspace_size")
+    ws = _byte_workspace(workspace, need.value, dev)
+    args = (_ptr(dresid_out, shape, like, "dresid_out"), _ptr(dnormed, shape, like, "dnormed"),
+            _ptr(resid_out, shape, like, "resid_out"), _ptr(y, shape, like, "y"), _ptr(weight, vec, like, "weight"),
+            _ptr(post_weight, vec, like, "post_weight"), _ptr(gate, vec, like, "gate"), scale, eps,
+            _ptr(dresid, shape, like, "dresid"), _ptr(dy, shape, like, "dy"), *ptrs, stride)
+    with torch.cuda.device(dev):
+        _check(_lib.bkmoo_residual_norm_backward(M, D, dt, K, rows, *args, ws.data_ptr(), ws.numel(),
+                                                 _stream_ptr(dev)), "bkmoo_residual_norm_backward")
+    return dresid, dy
+
+
+def ffn_workspace_size(M: int, D: int, F: int, dtype, backward: bool = False) -> int:
+    code = dtype if isinstance(dtype, int) else (F32 if dtype in (torch.float32, "f32") else BF16)
+    out = ctypes.c_size_t(0)
+    _check(_lib.bkmoo_ffn_workspace_size(M, D, F, code, int(backward), ctypes.byref(out)), "bkmoo_ffn_workspace_size")
+    return out.value
+
+
+def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, act: str = "silu",
+                save: bool = False, out: Optional[torch.Tensor] = None, gate_out: Optional[torch.Tensor] = None,
+                up_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gated feed-forward block: (y, u, v) with y = (act(u) * v) w_down^T, u = x w_gate^T,
+    v = x w_up^T for x [M, D], w_gate and w_up [F, D], w_down [D, F].  u and v, which
+    the backward pass needs, are None unless `save` is set or they are given."""
+    M, D, dt = _matrix(x, "x")
+    if w_gate.dim() != 2:
+        raise ValueError("w_gate must have two dimensions")
+    F, dev = w_gate.shape[0], x.device
+    if out is None:
+        out = torch.empty((M, D), dtype=x.dtype, device=dev)
+    if save and gate_out is None:
+        gate_out = torch.empty((M, F), dtype=x.dtype, device=dev)
+    if save and up_out is None:
+        up_out = torch.empty((M, F), dtype=x.dtype, device=dev)
+    ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, dt), dev)
+    args = (_ptr(x, (M, D), x, "x"), _ptr(w_gate, (F, D), x, "w_gate"), _ptr(w_up, (F, D), x, "w_up"),
+            _ptr(w_down, (D, F), x, "w_down"), _ptr(out, (M, D), x, "out"), _ptr(gate_out, (M, F), x, "gate_out"),
+            _ptr(up_out, (M, F), x, "up_out"))
+    with torch.cuda.device(dev):
+        _check(_lib.bkmoo_ffn_forward(M, D, F, dt, ACTS[act], *args, ws.data_ptr(), ws.numel(), _stream_ptr(dev)),
+               "bkmoo_ffn_forward")
+    return out, gate_out, up_out
+
+
+def ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate_out: torch.Tensor, up_out: torch.Tensor,
+                 w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, act: str = "silu",
+                 task_rows: Optional[Sequence[int]] = None, dw_gate: Optional[torch.Tensor] = None,
+                 dw_up: Optional[torch.Tensor] = None, dw_down: Optional[torch.Tensor] = None,
+                 dx: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradients of ffn_forward: returns dx and writes the K tasks' weight gradients to
+    dw_gate, dw_up and dw_down, each [K, D * F] with contiguous rows (columns of the
+    gradient buffer; a row is the flattened matrix).  task_rows: K + 1 offsets of the
+    tasks' rows in the batch."""
+    M, D, dt = _matrix(x, "x")
+    if w_gate.dim() != 2:
+        raise ValueError("w_gate must have two dimensions")
+    F, dev = w_gate.shape[0], x.device
+    rows, K = _task_rows(task_rows, M)
+    if dw_gate is None or dw_up is None or dw_down is None:
+        raise ValueError("dw_gate, dw_up and dw_down are needed")
+    ptrs, stride = _task_grads(((dw_gate, "dw_gate"), (dw_up, "dw_up"), (dw_down, "dw_down")), K, D * F, x)
+    if dx is None:
+        dx = torch.empty((M, D), dtype=x.dtype, device=dev)
+    ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, dt, True), dev)
+    args = (_ptr(dy, (M, D), x, "dy"), _ptr(x, (M, D), x, "x"), _ptr(gate_out, (M, F), x, "gate_out"),
+            _ptr(up_out, (M, F), x, "up_out"), _ptr(w_gate, (F, D), x, "w_gate"), _ptr(w_up, (F, D), x, "w_up"),
+            _ptr(w_down, (D, F), x, "w_down"), _ptr(dx, (M, D), x, "dx"), *ptrs, stride)
+    with torch.cuda.device(dev):
+        _check(_lib.bkmoo_ffn_backward(M, D, F, dt, ACTS[act], K, rows, *args, ws.data_ptr(), ws.numel(),
+                                       _stream_ptr(dev)), "bkmoo_ffn_backward")
+    return dx
+
+
+class AdamwTable:
+    """The addresses and sizes of adamw()'s tensors, in the order of the flat gradient.
+    N: their elements; blocks: their blocks of 256 elements (the scales of 8-bit moments)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], decay: Optional[Sequence[bool]] = None):
+        self.params = list(params)  # keeps their memory
+        if not self.params:
+            raise ValueError("no tensors")
+        self.dt, self.device = _dt(self.params[0]), _gpu(self.params[0], "parameters")
+        for p in self.params:
+            if p.dtype != self.params[0].dtype or p.device != self.device or not p.is_contiguous():
+                raise ValueError("parameters must be contiguous tensors of one dtype and device")
+        decay = [True] * len(self.params) if decay is None else list(decay)
+        if len(decay) != len(self.params):
+            raise ValueError("decay holds one entry for each tensor")
+        self.array = (_Tensor * len(self.params))(*[(p.data_ptr(), p.numel(), int(bool(d)))
+                                                    for p, d in zip(self.params, decay)])
+        self.N = sum(p.numel() for p in self.params)
+        n = ctypes.c_int64(0)
+        _check(_lib.bkmoo_adamw_blocks(len(self.params), self.array, ctypes.byref(n)), "bkmoo_adamw_blocks")
+        self.blocks = n.value
+
+
+def adamw_table(params: Sequence[torch.Tensor], decay: Optional[Sequence[bool]] = None) -> AdamwTable:
+    """Lay out adamw()'s tensors once (decay: whether weight decay applies, for each)."""
+    return AdamwTable(params, decay)
+
+
+def adamw(table: AdamwTable, grad: torch.Tensor, moment1: torch.Tensor, moment2: torch.Tensor, step: int,
+          lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+          master: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+          grad_scale: Optional[torch.Tensor] = None, seed: int = 0) -> None:
+    """One AdamW step over the table's tensors, in place.  grad [N]: float32 or bfloat16, the tensors'
+    gradients one after another (what resolve() returns).  moment1, moment2 [N]: float32, or
+    float8_e4m3fn with scales float32 [2, blocks] (zeros to start with).  master: float32 [N] copy of
+    bfloat16 parameters that takes the step.  grad_scale: float32 tensor of one element."""
+    dev, N = table.device, table.N
+    f8 = moment1.dtype == torch.float8_e4m3fn
+    sdt = torch.float8_e4m3fn if f8 else torch.float32
+    gp = _tensor(grad, (N,), grad.dtype, dev, "grad")
+    m1, m2 = _tensor(moment1, (N,), sdt, dev, "moment1"), _tensor(moment2, (N,), sdt, dev, "moment2")
+    if f8 != (scales is not None):
+        raise ValueError("scales go with 8-bit moments")
+    sc = None if scales is None else _tensor(scales, (2, table.blocks), torch.float32, dev, "scales")
+    mp = None if master is None else _tensor(master, (N,), torch.float32, dev, "master")
+    gs = None
+    if grad_scale is not None:
+        if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
+            raise ValueError(f"grad_scale must be one float32 value on {dev}")
+        gs = grad_scale.data_ptr()
+    hp = _AdamwHparams(lr, beta1, beta2, eps, weight_decay, step, seed & 0xFFFFFFFF)
+    with torch.cuda.device(dev):
+        _check(_lib.bkmoo_adamw(len(table.params), table.array, table.dt, N, gp, _dt(grad), STATE_F8 if f8 else STATE_F32,
+                                m1, m2, sc, table.blocks if f8 else 0, mp, ctypes.byref(hp), gs, _stream_ptr(dev)),
+               "bkmoo_adamw")

@@ -6,8 +6,8 @@ Every translation unit under csrc/ is compiled in parallel into _build/ and
 linked into paper_2606_05613_amd/libbkmoo.so.  All device code is built with
 packed-fp32 instruction selection disabled; the units holding the solvers
 (the solve and exact-solve kernels and the cooperative kernel that embeds
-them) and the conflict statistics additionally without floating-point
-contraction, so their scalar expressions round as written.
+them), the conflict statistics and the AdamW step additionally without
+floating-point contraction, so their scalar expressions round as written.
 
 After compiling, the generated gfx950 assembly is checked, and the build
 fails on either finding:
@@ -41,10 +41,11 @@ LIB = os.path.join(PKG, "libbkmoo.so")
 ARCH = "gfx950"
 
 SOURCES = ["api.hip", "schedule.hip", "gram.hip", "solve.hip", "solve_exact.hip", "combine.hip",
-           "hybrid.hip", "refill.hip", "conflicts.hip", "slices.hip"]
+           "hybrid.hip", "refill.hip", "conflicts.hip", "slices.hip",
+           "ffn.hip", "ffn_bf16.hip", "ffn_f32.hip", "norm.hip", "adamw.hip"]
 EXTRA = {"solve.hip": ["-ffp-contract=off"], "solve_exact.hip": ["-ffp-contract=off"],
          "hybrid.hip": ["-ffp-contract=off"], "refill.hip": ["-ffp-contract=off"],
-         "conflicts.hip": ["-ffp-contract=off"]}
+         "conflicts.hip": ["-ffp-contract=off"], "adamw.hip": ["-ffp-contract=off"]}
 
 
 def hipcc() -> str:

@@ -1,0 +1,99 @@
+// Element access of the layer operators: fp32 and bf16 in memory, fp32 in registers.
+#pragma once
+
+#include "internal.h"
+
+namespace bkmoo {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+// Element loads and stores of either type; four neighbours at once at any alignment.
+__device__ __forceinline__ float load1(const float *p) { return *p; }
+__device__ __forceinline__ float load1(const __bf16 *p) { return (float)*p; }
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+__device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4_any *)p; }
+__device__ __forceinline__ f32x4 load4(const __bf16 *p) {
+  return __builtin_convertvector((bf16x4)*(const bf16x4_any *)p, f32x4);
+}
+__device__ __forceinline__ void store4(float *p, f32x4 x) { *(f32x4_any *)p = x; }
+__device__ __forceinline__ void store4(__bf16 *p, f32x4 x) {
+  *(bf16x4_any *)p = __builtin_convertvector(x, bf16x4);
+}
+
+// The 16 bytes of a chunk that starts at element c of a row of `n` elements (any
+// alignment), zeros past the row's end.
+template <typename T>
+__device__ __forceinline__ u32x4 guarded_chunk(const T *row, int64_t c, int64_t n) {
+  constexpr int V = 16 / sizeof(T);
+  if (c + V <= n) return *(const u32x4_any *)(row + c);
+  union {
+    u32x4 v;
+    uint32_t w[4];
+    uint16_t h[8];
+  } x;
+  x.v = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (c + e < n) {
+      if (sizeof(T) == 2)
+        x.h[e] = ((const uint16_t *)row)[c + e];
+      else
+        x.w[e] = ((const uint32_t *)row)[c + e];
+    }
+  return x.v;
+}
+
+// Vectors of 16 bytes as fp32 and back (rounded to nearest even).
+template <typename T>
+struct Vec {
+  static constexpr int kN = 16 / sizeof(T);
+};
+__device__ __forceinline__ void unpack(u32x4 v, float (&x)[4]) {
+  x[0] = __uint_as_float(v.x);
+  x[1] = __uint_as_float(v.y);
+  x[2] = __uint_as_float(v.z);
+  x[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ void unpack(u32x4 v, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(v[i] << 16);
+    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ u32x4 pack(const float (&x)[4]) {
+  return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+}
+__device__ __forceinline__ u32x4 pack(const float (&x)[8]) {
+  union {
+    bf16x8 h;
+    u32x4 v;
+  } u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u.h[i] = (__bf16)x[i];
+  return u.v;
+}
+// The 16 bytes at element c of a row of n elements: what lies past its end stays as it is.
+template <typename T>
+__device__ __forceinline__ void guarded_store(T *row, int64_t c, int64_t n, u32x4 v) {
+  constexpr int V = 16 / sizeof(T);
+  if (c + V <= n) {
+    *(u32x4_any *)(row + c) = v;
+    return;
+  }
+  union {
+    u32x4 v;
+    T e[V];
+  } x;
+  x.v = v;
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (c + e < n) row[c + e] = x.e[e];
+}
+
+}  // namespace bkmoo

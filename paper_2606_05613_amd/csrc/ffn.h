@@ -1,0 +1,35 @@
+// The gated feed-forward block's products: shared by its launchers and kernels.
+#pragma once
+
+#include "internal.h"
+
+namespace bkmoo {
+
+enum GateAct : int { kSilu = 0, kGelu = 1 };
+
+// The tiled products.  x, y [M][D]; u, v, h [M][F]; Wg, Wu [F][D]; Wd [D][F].
+enum Mode : int {
+  kGateUp,      // u = x Wg^T, v = x Wu^T -> h = a(u) v (and u, v)
+  kDown,        // y = h Wd^T
+  kHiddenGrad,  // dh = dy Wd -> du = dh v a'(u), dv = dh a(u), h = a(u) v
+  kInputGrad,   // dx = du Wg + dv Wu
+  kWeightGrad   // per task: dWg = du^T x, dWu = dv^T x, dWd = dy^T h
+};
+
+struct TileArgs {
+  const void *a[3], *b[3];  // operands (kWeightGrad: of the three matrices)
+  void *out[3];
+  const void *u, *v;        // kHiddenGrad
+  float *partial;           // [splits][M][N], where the sum is split
+  int64_t M, N, K;          // output rows and columns (kWeightGrad: of the first two matrices), length of the sum
+  int64_t task_stride;      // elements from one task's gradient row to the next
+  int tiles_m, tiles_n, splits, act;
+  int64_t rows[kMaxK + 1];  // kWeightGrad: the tasks' rows
+};
+
+hipError_t launch_ffn_tile_f32(Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s);
+hipError_t launch_ffn_tile_bf16(Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s);
+// aligned: operands start at 16 bytes and so do all their rows.  wide: 256 x 256 tiles.
+hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s);
+
+}  // namespace bkmoo

@@ -1,0 +1,48 @@
+// The launcher of one element type's tiled products.
+#pragma once
+
+#include "ffn_tile.h"
+
+namespace bkmoo {
+
+// 256 x 256 tiles on eight waves, or 128 x 128 on four: see ffn_wide_tiles().
+template <typename T, Mode MODE, bool ALIGNED>
+hipError_t launch_mode(TileArgs g, int tasks, bool wide, hipStream_t s) {
+  const int64_t rows = g.M, cols = MODE == kGateUp ? 2 * g.N : g.N;
+  const int side = wide ? 256 : 128;
+  g.tiles_m = (int)((rows + side - 1) / side);
+  g.tiles_n = (int)((cols + side - 1) / side);
+  const int64_t probs = MODE == kWeightGrad ? 3 * tasks : g.splits > 1 ? g.splits : 1;
+  const int64_t n = (int64_t)g.tiles_m * g.tiles_n * probs;
+  if (n == 0) return hipSuccess;
+  if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if constexpr (ALIGNED) {
+    if (wide) {
+      ffn_tile_kernel<T, MODE, 256, 256, 2, 4, true><<<dim3((unsigned)n), dim3(512), 0, s>>>(g);
+      return hipGetLastError();
+    }
+  }
+  ffn_tile_kernel<T, MODE, 128, 128, 2, 2, ALIGNED><<<dim3((unsigned)n), dim3(256), 0, s>>>(g);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_ffn_tile_of(Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s) {
+  switch (mode) {
+    case kGateUp:
+      return aligned ? launch_mode<T, kGateUp, true>(g, tasks, wide, s) : launch_mode<T, kGateUp, false>(g, tasks, false, s);
+    case kDown:
+      return aligned ? launch_mode<T, kDown, true>(g, tasks, wide, s) : launch_mode<T, kDown, false>(g, tasks, false, s);
+    case kHiddenGrad:
+      return aligned ? launch_mode<T, kHiddenGrad, true>(g, tasks, wide, s)
+                     : launch_mode<T, kHiddenGrad, false>(g, tasks, false, s);
+    case kInputGrad:
+      return aligned ? launch_mode<T, kInputGrad, true>(g, tasks, wide, s)
+                     : launch_mode<T, kInputGrad, false>(g, tasks, false, s);
+    default:
+      return aligned ? launch_mode<T, kWeightGrad, true>(g, tasks, wide, s)
+                     : launch_mode<T, kWeightGrad, false>(g, tasks, false, s);
+  }
+}
+
+}  // namespace bkmoo
