@@ -8,12 +8,15 @@
 // (Mode), so that the gate's activation, its product and their derivatives
 // never travel through memory as fp32.
 //
-// A workgroup computes a BM x BN tile.  It takes steps of 128 bytes along k
-// through two LDS buffers: while the waves multiply step t, step t + 1 travels
-// from memory straight into the other buffer (buffer loads with the LDS as their
-// destination: no registers, no LDS write instructions), and one barrier a step
-// hands it over.  Rows past the end of a matrix fall outside the descriptor's
-// range and arrive as zeros; so do the chunks past K of a K-contiguous operand.
+// A workgroup computes a BM x BN tile in steps of 128 bytes along k through two LDS
+// buffers, filled straight from memory (buffer loads with the LDS as their destination:
+// no registers, no LDS write instructions).  While the first half of step t is multiplied
+// the second half's fragments are read into registers; then one barrier, behind which
+// step t's buffer is refilled with step t + 2 and the first half of step t + 1 is read
+// while the second half of step t is multiplied: the barrier finds every wave with its
+// next operands in registers.  Rows past the end of a matrix fall outside the
+// descriptor's range and arrive as zeros; so do the chunks past K of a K-contiguous
+// operand.
 //
 // LDS layouts (16-byte chunks; the loads fill LDS in lane order, so a layout is
 // made by choosing what each lane reads):
@@ -105,9 +108,10 @@ struct Stage {
   static __device__ __forceinline__ bool second(int wave, int i) { return ((wave * kPer + i) >> 2) & 1; }
 };
 
+// A buffer descriptor of the `bytes` (>= 0) from p on; its range ends at 2 GiB.
 __device__ __forceinline__ i32x4 make_desc(const void *p, int64_t bytes) {
   const uint64_t a = (uint64_t)p;
-  const int64_t n = bytes < 0 ? 0 : bytes < 0x7fffffff ? bytes : 0x7fffffff;
+  const uint32_t n = (uint32_t)((uint64_t)bytes >> 31) != 0 ? 0x7fffffffu : (uint32_t)bytes;
   i32x4 r;
   r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
   r.y = __builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffff));
@@ -125,7 +129,12 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, i32x4 desc, uint32_t o
                : "s"(lds), "v"(off), "s"(desc)
                : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Until at most N of the wave's loads are outstanding.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 // Every wave's LDS reads have returned and its LDS writes are done.
 __device__ __forceinline__ void barrier_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -139,7 +148,7 @@ struct Source {
   int64_t ld, rows;
 };
 
-// Fragments: 16 rows (or columns) of an operand and 64 bytes of k.
+// Fragments: 16 rows (or columns) of an operand, half a step of k.
 template <typename T>
 struct Frag;
 template <>
@@ -153,8 +162,7 @@ struct Frag<float> {
 
 template <typename T, int W, bool KC>
 struct Reader {
-  uint32_t base[2];
-  uint32_t x;
+  uint32_t base[2], x;
   // first: the wave's first row in the tile
   __device__ __forceinline__ Reader(int first, int lane) {
     const int g = lane >> 4, j = lane & 15;
@@ -166,33 +174,35 @@ struct Reader {
     } else if constexpr (sizeof(T) == 2) {
       const int k = 8 * g + (j >> 2);
       base[0] = (uint32_t)(k * W * 2 + 8 * (j & 3));
-      base[1] = 0;
       x = (uint32_t)(32 * ((j >> 2) | ((g & 1) << 2))) ^ (uint32_t)(first * 2);
     } else {
       base[0] = (uint32_t)(4 * g * W * 4 + 4 * j);
-      base[1] = 0;
       x = (uint32_t)(64 * g) ^ (uint32_t)(first * 4);
     }
   }
-  // Fragment i of half kk of the step at LDS address `lds`.
-  __device__ __forceinline__ Frag<T> read(uint32_t lds, int kk, int i) const {
+  // (a pointer, so that what is added to it becomes the instruction's offset)
+  static __device__ __forceinline__ const BKMOO_LDS char *at(uint32_t a) {
+    return (const BKMOO_LDS char *)(uintptr_t)a;
+  }
+  // Fragment i of a half of the step at LDS address `lds`.
+  __device__ __forceinline__ Frag<T> read(uint32_t lds, int half, int i) const {
     Frag<T> f;
     if constexpr (KC) {
-      f.v = *(const BKMOO_LDS decltype(f.v) *)(uintptr_t)(lds + base[kk] + i * 16 * 128);
+      f.v = *(const BKMOO_LDS decltype(f.v) *)(at(lds + base[half]) + i * 16 * 128);
     } else if constexpr (sizeof(T) == 2) {
-      const uint32_t a = lds + base[0] + (x ^ (uint32_t)(i * 32)) + kk * 32 * W * 2;
+      const BKMOO_LDS char *a = at(lds + base[0] + (x ^ (uint32_t)(i * 32))) + half * 32 * W * 2;
       union {
         s16x4 h[2];
         bf16x8 v;
       } u;
-      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((BKMOO_LDS s16x4 *)(uintptr_t)a);
-      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((BKMOO_LDS s16x4 *)(uintptr_t)(a + 4 * W * 2));
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((BKMOO_LDS s16x4 *)a);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((BKMOO_LDS s16x4 *)(a + 4 * W * 2));
       f.v = u.v;
     } else {
-      // rows 16 kk + 4 g + e: their place depends on g alone
-      const uint32_t a = lds + base[0] + (x ^ (uint32_t)(i * 64)) + kk * 16 * W * 4;
+      // rows 16 half + 4 g + e: their place depends on g alone
+      const BKMOO_LDS char *a = at(lds + base[0] + (x ^ (uint32_t)(i * 64))) + half * 16 * W * 4;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f.v[e] = *(const BKMOO_LDS float *)(uintptr_t)(a + e * W * 4);
+      for (int e = 0; e < 4; ++e) f.v[e] = *(const BKMOO_LDS float *)(a + e * W * 4);
     }
     return f;
   }
@@ -295,40 +305,74 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
   SA::template offsets<false>(wave, lane, a[0].ld, aoff);
   SB::template offsets<GU>(wave, lane, b[0].ld, boff);
 
-  // step t to LDS buffer `buf` (ALIGNED)
-  auto load = [&](int t, int buf) {
+  // Where the next step to load starts, and the bytes from there to its matrix's
+  // end (ALIGNED); none after the last step, so that its loads bring zeros.
+  struct Next {
+    const char *a, *b, *b2;
+    int64_t abytes, bbytes;
+    int left, t;  // of the segment's sum; step
+  } nx;
+  const int64_t astep = AKC ? 128 : (int64_t)BK * a[0].ld * ES, bstep = BKC ? 128 : (int64_t)BK * b[0].ld * ES;
+  auto start_at = [&](int t) {
     const int seg = MODE == kInputGrad && t >= steps_seg ? 1 : 0;
     const int64_t k0 = (int64_t)(t - seg * steps_seg) * BK;
     const Source<T> &A = seg ? a[1] : a[0];
     const Source<T> &B = seg ? b[1] : b[0];
     const int64_t ea = AKC ? m0 * A.ld + k0 : k0 * A.ld + m0;
     const int64_t eb = BKC ? n0 * B.ld + k0 : k0 * B.ld + n0;
-    const i32x4 da = make_desc(A.p + ea, (A.rows * A.ld - ea) * ES);
-    const i32x4 db = make_desc(B.p + eb, (B.rows * B.ld - eb) * ES);
-    i32x4 db2 = db;
-    if constexpr (GU) db2 = make_desc(b[1].p + eb, (b[1].rows * b[1].ld - eb) * ES);
-    const uint32_t la = lds0 + buf * kStep + wave * SA::kPer * 1024;
-    const uint32_t lb = lds0 + buf * kStep + SA::kBytes + wave * SB::kPer * 1024;
-    const bool tail = K - k0 < BK;
-#pragma unroll
-    for (int i = 0; i < SA::kPer; ++i) {
+    nx.a = (const char *)(A.p + ea);
+    nx.b = (const char *)(B.p + eb);
+    nx.b2 = GU ? (const char *)(b[1].p + eb) : nx.b;
+    nx.abytes = (A.rows * A.ld - ea) * ES;
+    nx.bbytes = (B.rows * B.ld - eb) * ES;
+    nx.left = (int)(K - k0);
+    nx.t = t;
+  };
+  struct Step {
+    i32x4 a, b, b2;
+    uint32_t la, lb;
+    int left;
+  };
+  auto next_step = [&](int buf) {
+    Step x;
+    x.a = make_desc(nx.a, nx.abytes);
+    x.b = make_desc(nx.b, nx.bbytes);
+    x.b2 = GU ? make_desc(nx.b2, nx.bbytes) : x.b;
+    x.la = lds0 + buf * kStep + wave * SA::kPer * 1024;
+    x.lb = lds0 + buf * kStep + SA::kBytes + wave * SB::kPer * 1024;
+    x.left = nx.left;
+    nx.a += astep;
+    nx.b += bstep;
+    nx.b2 += bstep;
+    nx.abytes -= astep;
+    nx.bbytes -= bstep;
+    nx.left -= BK;
+    ++nx.t;
+    if (nx.t >= t1)
+      nx.abytes = nx.bbytes = 0;
+    else if (MODE == kInputGrad && nx.t == steps_seg)
+      start_at(nx.t);
+    return x;
+  };
+  constexpr int kLoads = SA::kPer + SB::kPer;
+  auto piece = [&](const Step &x, int i) {
+    if (i < SA::kPer) {
       uint32_t off = aoff[i];
-      if (AKC && tail) {
+      if (AKC && x.left < BK) {
         int row, chunk;
         SA::place(wave * SA::kPer + i, lane, row, chunk);
-        if (k0 + chunk * (16 / ES) >= K) off = kNowhere;
+        if (chunk * (16 / ES) >= x.left) off = kNowhere;
       }
-      load_to_lds(la + i * 1024, da, off);
-    }
-#pragma unroll
-    for (int i = 0; i < SB::kPer; ++i) {
-      uint32_t off = boff[i];
-      if (BKC && tail) {
+      load_to_lds(x.la + i * 1024, x.a, off);
+    } else {
+      const int q = i - SA::kPer;
+      uint32_t off = boff[q];
+      if (BKC && x.left < BK) {
         int row, chunk;
-        SB::place(wave * SB::kPer + i, lane, row, chunk);
-        if (k0 + chunk * (16 / ES) >= K) off = kNowhere;
+        SB::place(wave * SB::kPer + q, lane, row, chunk);
+        if (chunk * (16 / ES) >= x.left) off = kNowhere;
       }
-      load_to_lds(lb + i * 1024, GU && SB::second(wave, i) ? db2 : db, off);
+      load_to_lds(x.lb + q * 1024, GU && SB::second(wave, q) ? x.b2 : x.b, off);
     }
   };
 
@@ -357,10 +401,10 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
       }
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](int slot) {
     if constexpr (!ALIGNED) {
-      const uint32_t la = lds0 + buf * kStep + wave * SA::kPer * 1024 + lane * 16;
-      const uint32_t lb = lds0 + buf * kStep + SA::kBytes + wave * SB::kPer * 1024 + lane * 16;
+      const uint32_t la = lds0 + slot * kStep + wave * SA::kPer * 1024 + lane * 16;
+      const uint32_t lb = lds0 + slot * kStep + SA::kBytes + wave * SB::kPer * 1024 + lane * 16;
 #pragma unroll
       for (int i = 0; i < SA::kPer; ++i) *(BKMOO_LDS u32x4 *)(uintptr_t)(la + i * 1024) = ra[i];
 #pragma unroll
@@ -378,40 +422,76 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
   const Reader<T, BM, AKC> reada(wm * TM * 16, lane);
   const Reader<T, BN, BKC> readb(wn * TN * 16, lane);
 
-  if (t0 < t1) {
-    if (ALIGNED) {
-      load(t0, 0);
+  // Fragments of both halves of a step: one is multiplied while the other is read.
+  Frag<T> fa[2][TM], fb[2][TN];
+  auto read = [&](int half, int buf, int i) {
+    const uint32_t la = lds0 + buf * kStep;
+    if (i < TN)
+      fb[half][i] = readb.read(la + SA::kBytes, half, i);
+    else
+      fa[half][i - TN] = reada.read(la, half, i - TN);
+  };
+  // The products of a half, row by row of pieces, with the reads of the other half (of
+  // the step in LDS buffer `buf`) and, LOAD, the loads of a step in between: none holds up
+  // another, and every read has arrived when the half ends.
+  auto work = [&]<int HALF, bool LOAD>(int buf, const Step &x) {
+    constexpr int kReads = TM + TN, kEach = (kReads + TM - 3) / (TM - 2), kLoadEach = 2 * kLoads / TM;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+      for (int q = i * kEach; q < (i + 1) * kEach; ++q)
+        if (q < kReads) read(HALF ^ 1, buf, q);
+      if constexpr (LOAD)
+#pragma unroll
+        for (int q = i * kLoadEach; q < (i + 1) * kLoadEach; ++q)
+          if (q < kLoads) piece(x, q);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  const int n = t1 - t0;
+  Step x = {};
+  if (n > 0) {
+    if constexpr (ALIGNED) {
+      start_at(t0);
+      x = next_step(0);
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) piece(x, q);
+      x = next_step(1);
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) piece(x, q);
+      wait_loads<kLoads>();
     } else {
       fetch(t0);
       put(0);
+      if (n > 1) {
+        fetch(t0 + 1);
+        put(1);
+      }
     }
-  }
-  for (int t = t0; t < t1; ++t) {
-    const int buf = (t - t0) & 1;
-    // step t has arrived, and nobody reads the other buffer any more
-    if (ALIGNED) wait_loads();
     barrier_lds();
-    if (t + 1 < t1) {
-      if (ALIGNED)
-        load(t + 1, buf ^ 1);
-      else
-        fetch(t + 1);
-    }
-    const uint32_t la = lds0 + buf * kStep, lb = la + SA::kBytes;
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      Frag<T> fa[TM], fb[TN];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) fb[j] = readb.read(lb, kk, j);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) fa[i] = reada.read(la, kk, i);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
-    }
-    if (!ALIGNED && t + 1 < t1) put(buf ^ 1);
+    for (int i = 0; i < TM + TN; ++i) read(0, 0, i);
   }
+  for (int t = 0; t < n; ++t) {
+    const int buf = t & 1;
+    if constexpr (ALIGNED)
+      x = next_step(buf);
+    else if (t + 2 < n)
+      fetch(t0 + t + 2);
+    work.template operator()<0, false>(buf, x);
+    // Step t is in registers and step t + 1 in LDS, for every wave: step t's
+    // buffer is free.
+    if constexpr (ALIGNED) wait_loads<0>();
+    barrier_lds();
+    work.template operator()<1, ALIGNED>(buf ^ 1, x);  // (after the last step: reads what is there, not used)
+    if constexpr (!ALIGNED)
+      if (t + 2 < n) put(buf);
+    asm volatile("" ::: "memory");  // the reads stay in this iteration
+  }
+  if constexpr (ALIGNED) wait_loads<0>();
 
   // lane: row m of piece i, four columns from n of piece j
   const int64_t mrow = m0 + wm * TM * 16 + (lane & 15);
