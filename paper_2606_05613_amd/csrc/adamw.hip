@@ -59,45 +59,28 @@ struct AdamArgs {
 };
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 
-typedef u32x4 u32x4_byte __attribute__((aligned(1)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_byte __attribute__((aligned(1)));
 
 // Eight elements from i on, of n; zeros past the end.
-__device__ __forceinline__ void load8(const float *p, int64_t i, int64_t n, float (&x)[8]) {
+template <typename T>
+__device__ __forceinline__ void load8_of(const T *p, int64_t i, int64_t n, float (&x)[8]) {
   if (i + 8 <= n) {
-    const u32x4 a = *(const u32x4_byte *)(p + i), b = *(const u32x4_byte *)(p + i + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[e] = __uint_as_float(a[e]);
-      x[e + 4] = __uint_as_float(b[e]);
-    }
+    load8(p + i).get(x);
     return;
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = i + e < n ? p[i + e] : 0.0f;
+  for (int e = 0; e < 8; ++e) x[e] = i + e < n ? load1(p + i + e) : 0.0f;
 }
-__device__ __forceinline__ void load8(const __bf16 *p, int64_t i, int64_t n, float (&x)[8]) {
-  unpack(guarded_chunk(p, i, n), x);
-}
-__device__ __forceinline__ void store8(float *p, int64_t i, int64_t n, const float (&x)[8]) {
+template <typename T>
+__device__ __forceinline__ void store8_of(T *p, int64_t i, int64_t n, const float (&x)[8]) {
   if (i + 8 <= n) {
-    u32x4 a, b;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      a[e] = __float_as_uint(x[e]);
-      b[e] = __float_as_uint(x[e + 4]);
-    }
-    *(u32x4_byte *)(p + i) = a;
-    *(u32x4_byte *)(p + i + 4) = b;
+    store8(p + i, x);
     return;
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (i + e < n) p[i + e] = x[e];
-}
-__device__ __forceinline__ void store8(__bf16 *p, int64_t i, int64_t n, const float (&x)[8]) {
-  guarded_store(p, i, n, pack(x));
+    if (i + e < n) p[i + e] = (T)x[e];
 }
 
 // Eight e4m3 values.
@@ -184,11 +167,11 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
     const int64_t i = base + threadIdx.x * kLaneElems;
     if (!S8 && i >= n) break;
     float g[8], m[8], q[8], x[8];
-    load8(grad, i, n, g);
+    load8_of(grad, i, n, g);
     if constexpr (MASTER)
-      load8(master, i, n, x);
+      load8_of(master, i, n, x);
     else
-      load8((const T *)p, i, n, x);
+      load8_of((const T *)p, i, n, x);
     if constexpr (S8) {
       uint8_t *m8 = (uint8_t *)a.m + start, *v8 = (uint8_t *)a.v + start;
       const int64_t blk = a.block[t] + i / kBlock;
@@ -248,24 +231,24 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
       }
     } else {
       float *m32 = (float *)a.m + start, *v32 = (float *)a.v + start;
-      load8(m32, i, n, m);
-      load8(v32, i, n, q);
+      load8_of(m32, i, n, m);
+      load8_of(v32, i, n, q);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float ge = g[e] * gs;
         m[e] = a.b1 * m[e] + a.c1 * ge;
         q[e] = a.b2 * q[e] + a.c2 * (ge * ge);
       }
-      store8(m32, i, n, m);
-      store8(v32, i, n, q);
+      store8_of(m32, i, n, m);
+      store8_of(v32, i, n, q);
 #pragma unroll
       for (int e = 0; e < 8; ++e) q[e] = sqrtf(q[e]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = x[e] * keep - a.step * m[e] / (q[e] * a.rootc + a.eps);
     if (i < n) {
-      if constexpr (MASTER) store8(master, i, n, x);
-      store8(p, i, n, x);
+      if constexpr (MASTER) store8_of(master, i, n, x);
+      store8_of(p, i, n, x);
     }
   }
 }

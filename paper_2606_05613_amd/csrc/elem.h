@@ -11,19 +11,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-// Element loads and stores of either type; four neighbours at once at any alignment.
 __device__ __forceinline__ float load1(const float *p) { return *p; }
 __device__ __forceinline__ float load1(const __bf16 *p) { return (float)*p; }
-typedef f32x4 f32x4_any __attribute__((aligned(4)));
-typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
-__device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4_any *)p; }
-__device__ __forceinline__ f32x4 load4(const __bf16 *p) {
-  return __builtin_convertvector((bf16x4)*(const bf16x4_any *)p, f32x4);
-}
-__device__ __forceinline__ void store4(float *p, f32x4 x) { *(f32x4_any *)p = x; }
-__device__ __forceinline__ void store4(__bf16 *p, f32x4 x) {
-  *(bf16x4_any *)p = __builtin_convertvector(x, bf16x4);
-}
 
 // The 16 bytes of a chunk that starts at element c of a row of `n` elements (any
 // alignment), zeros past the row's end.
@@ -78,6 +67,41 @@ __device__ __forceinline__ u32x4 pack(const float (&x)[8]) {
   for (int i = 0; i < 8; ++i) u.h[i] = (__bf16)x[i];
   return u.v;
 }
+// Eight consecutive elements at any alignment.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<float> {
+  u32x4 a, b;
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = __uint_as_float(a[e]);
+      x[e + 4] = __uint_as_float(b[e]);
+    }
+  }
+};
+template <>
+struct Eight<__bf16> {
+  u32x4 v;
+  __device__ __forceinline__ void get(float (&x)[8]) const { unpack(v, x); }
+};
+__device__ __forceinline__ Eight<float> load8(const float *p) {
+  return {*(const u32x4_any *)p, *(const u32x4_any *)(p + 4)};
+}
+__device__ __forceinline__ Eight<__bf16> load8(const __bf16 *p) { return {*(const u32x4_any *)p}; }
+__device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
+  u32x4 a, b;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    a[e] = __float_as_uint(x[e]);
+    b[e] = __float_as_uint(x[e + 4]);
+  }
+  *(u32x4_any *)p = a;
+  *(u32x4_any *)(p + 4) = b;
+}
+__device__ __forceinline__ void store8(__bf16 *p, const float (&x)[8]) { *(u32x4_any *)p = pack(x); }
+
 // The 16 bytes at element c of a row of n elements: what lies past its end stays as it is.
 template <typename T>
 __device__ __forceinline__ void guarded_store(T *row, int64_t c, int64_t n, u32x4 v) {

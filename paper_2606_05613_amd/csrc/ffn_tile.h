@@ -32,6 +32,8 @@
 // consecutive n of one row m: 8- or 16-byte stores.
 #pragma once
 
+#include <type_traits>
+
 #include "elem.h"
 #include "ffn.h"
 
@@ -42,23 +44,33 @@ namespace bkmoo {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// Gate activation and its derivative.
-__device__ __forceinline__ float gate_act(float u, int act) {
-  if (act == kSilu) return u / (1.0f + expf(-u));
-  // GELU's tanh form: u times the logistic function of twice tanh's argument
-  const float z = 1.5957691216057308f * (u + 0.044715f * u * u * u);
-  return u / (1.0f + expf(-z));
+// Gate activation and its derivative: z s(z') with the logistic function s (GELU's tanh
+// form is u times s of twice tanh's argument).  One exponential of a non-positive
+// number gives s and 1 - s without cancellation.  bf16: the exponential and reciprocal
+// instructions (an ulp or two of fp32) are far below the result's rounding.
+template <typename T>
+__device__ __forceinline__ void logistic(float z, float &s, float &r) {
+  const float e = sizeof(T) == 2 ? __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(z)) : expf(-fabsf(z));
+  const float p = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
+  s = z >= 0.0f ? p : e * p;
+  r = z >= 0.0f ? e * p : p;
+  if (!(z == z)) s = r = z;
 }
+template <typename T>
+__device__ __forceinline__ float gate_act(float u, int act) {
+  float s, r;
+  logistic<T>(act == kSilu ? u : 1.5957691216057308f * (u + 0.044715f * u * u * u), s, r);
+  return u * s;
+}
+template <typename T>
 __device__ __forceinline__ void gate_act_grad(float u, int act, float &a, float &da) {
-  float z = u, dz = 1.0f;
+  float z = u, dz = 1.0f, s, r;
   if (act != kSilu) {
     z = 1.5957691216057308f * (u + 0.044715f * u * u * u);
     dz = 1.5957691216057308f * (1.0f + 0.134145f * u * u);
   }
-  const float s = 1.0f / (1.0f + expf(-z));
+  logistic<T>(z, s, r);
   a = u * s;
-  // u s (1 - s) dz: 1 - s as the logistic function of -z, exact for large z
-  const float r = 1.0f / (1.0f + expf(z));
   const float q = s * r;
   da = q == 0.0f ? s : s + u * q * dz;
 }
@@ -90,22 +102,26 @@ struct Stage {
       chunk = p ^ (4 * ((row >> 2) & 3));
   }
 
-  // Byte offsets of the wave's pieces from the step's first element.  GU: the
-  // rows are 32 of one matrix and 32 of another in turn; the offset is in the
+  // Byte offsets of the wave's pieces from the step's first element.  HALF > 0: the
+  // rows are HALF of one matrix and HALF of another in turn; the offset is in the
   // row's own matrix.
-  template <bool GU>
+  template <int HALF>
   static __device__ __forceinline__ void offsets(int wave, int lane, int64_t ld, uint32_t *off) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       int row, chunk;
       place(wave * kPer + i, lane, row, chunk);
-      if (GU) row = (row >> 6) * 32 + (row & 31);
+      if (HALF > 0) row = row / (2 * HALF) * HALF + row % HALF;
       off[i] = (uint32_t)row * (uint32_t)(ld * kES) + (uint32_t)chunk * 16;
     }
   }
 
-  // Piece i reads the second matrix (GU).
-  static __device__ __forceinline__ bool second(int wave, int i) { return ((wave * kPer + i) >> 2) & 1; }
+  // Piece i (eight rows) reads the second matrix.
+  template <int HALF>
+  static __device__ __forceinline__ bool second(int wave, int i) {
+    if constexpr (HALF > 0) return ((wave * kPer + i) * 8 / HALF) & 1;
+    return false;
+  }
 };
 
 // A buffer descriptor of the `bytes` (>= 0) from p on; its range ends at 2 GiB.
@@ -113,9 +129,9 @@ __device__ __forceinline__ i32x4 make_desc(const void *p, int64_t bytes) {
   const uint64_t a = (uint64_t)p;
   const uint32_t n = (uint32_t)((uint64_t)bytes >> 31) != 0 ? 0x7fffffffu : (uint32_t)bytes;
   i32x4 r;
-  r.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)a);
-  r.y = __builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xffff));
-  r.z = __builtin_amdgcn_readfirstlane((int)n);
+  r.x = (int)(uint32_t)a;
+  r.y = (int)((uint32_t)(a >> 32) & 0xffff);
+  r.z = (int)n;
   r.w = 0x00020000;
   return r;
 }
@@ -123,7 +139,9 @@ __device__ __forceinline__ i32x4 make_desc(const void *p, int64_t bytes) {
 // 16 bytes a lane from memory to LDS at `lds` + 16 * lane; beyond the descriptor's
 // range zeros.  No register is written: what it leaves outstanding is waited for
 // by wait_loads() alone.  (M0 holds the LDS address; nothing else here uses it.)
-__device__ __forceinline__ void load_to_lds(uint32_t lds, i32x4 desc, uint32_t off) {
+__device__ __forceinline__ void load_to_lds(uint32_t lds, i32x4 d, uint32_t off) {
+  const i32x4 desc = {__builtin_amdgcn_readfirstlane(d.x), __builtin_amdgcn_readfirstlane(d.y),
+                      __builtin_amdgcn_readfirstlane(d.z), __builtin_amdgcn_readfirstlane(d.w)};
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(lds), "v"(off), "s"(desc)
@@ -217,6 +235,18 @@ __device__ __forceinline__ f32x4 multiply(const Frag<float> &n, const Frag<float
   return acc;
 }
 
+// A lane holds four columns, from 4 (lane / 16) on, of each of two neighbouring 16 x 16
+// pieces.  Sixteen-lane rows 1 and 3 of the first trade places with rows 0 and 2 of the
+// second: eight consecutive columns, from 16 (lane / 16 mod 2) + 8 (lane / 32) on.
+__device__ __forceinline__ void eight_columns(f32x4 a, f32x4 b, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a[e]), __float_as_uint(b[e]), false, false);
+    x[e] = __uint_as_float(r[0]);
+    x[e + 4] = __uint_as_float(r[1]);
+  }
+}
+
 // Tile number -> (row of tiles, column of tiles).  Workgroups go to the eight
 // XCDs in turn; each XCD gets a run of consecutive numbers, and consecutive
 // numbers cover patches of kPatch rows of tiles, so that the tiles in flight on
@@ -245,7 +275,8 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
   constexpr int BK = SA::kBK, ES = sizeof(T);
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 pieces of a wave's tile
   constexpr int kStep = SA::kBytes + SB::kBytes;
-  static_assert(!GU || BN / WN == 64, "a wave holds 32 columns of the gate and the same 32 of the up product");
+  // a wave holds kHalf columns of the gate and the same kHalf of the up product
+  constexpr int kHalf = GU ? BN / WN / 2 : 0;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStep];
 
   const int lane = threadIdx.x & 63;
@@ -302,8 +333,8 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(BKMOO_LDS unsigned char *)lds;
   uint32_t aoff[SA::kPer], boff[SB::kPer];
-  SA::template offsets<false>(wave, lane, a[0].ld, aoff);
-  SB::template offsets<GU>(wave, lane, b[0].ld, boff);
+  SA::template offsets<0>(wave, lane, a[0].ld, aoff);
+  SB::template offsets<kHalf>(wave, lane, b[0].ld, boff);
 
   // Where the next step to load starts, and the bytes from there to its matrix's
   // end (ALIGNED); none after the last step, so that its loads bring zeros.
@@ -372,7 +403,7 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
         SB::place(wave * SB::kPer + q, lane, row, chunk);
         if (chunk * (16 / ES) >= x.left) off = kNowhere;
       }
-      load_to_lds(x.lb + q * 1024, GU && SB::second(wave, q) ? x.b2 : x.b, off);
+      load_to_lds(x.lb + q * 1024, SB::template second<kHalf>(wave, q) ? x.b2 : x.b, off);
     }
   };
 
@@ -394,8 +425,8 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
       for (int i = 0; i < SB::kPer; ++i) {
         int row, chunk;
         SB::place(wave * SB::kPer + i, lane, row, chunk);
-        const Source<T> &B = (GU ? SB::second(wave, i) : seg != 0) ? b[1] : b[0];
-        if (GU) row = (row >> 6) * 32 + (row & 31);
+        const Source<T> &B = (GU ? SB::template second<kHalf>(wave, i) : seg != 0) ? b[1] : b[0];
+        if constexpr (GU) row = row / (2 * kHalf) * kHalf + row % kHalf;
         const int64_t r = (BKC ? n0 : k0) + row, c = (BKC ? k0 : n0) + chunk * (16 / ES);
         rb[i] = r < B.rows ? guarded_chunk(B.p + r * B.ld, c, B.ld) : u32x4{0, 0, 0, 0};
       }
@@ -422,6 +453,8 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
   const Reader<T, BM, AKC> reada(wm * TM * 16, lane);
   const Reader<T, BN, BKC> readb(wn * TN * 16, lane);
 
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, 1>;
   // Fragments of both halves of a step: one is multiplied while the other is read.
   Frag<T> fa[2][TM], fb[2][TN];
   auto read = [&](int half, int buf, int i) {
@@ -434,7 +467,9 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
   // The products of a half, row by row of pieces, with the reads of the other half (of
   // the step in LDS buffer `buf`) and, LOAD, the loads of a step in between: none holds up
   // another, and every read has arrived when the half ends.
-  auto work = [&]<int HALF, bool LOAD>(int buf, const Step &x) {
+  auto work = [&](auto half, auto loads, int buf, const Step &x) {
+    constexpr int HALF = decltype(half)::value;
+    constexpr bool LOAD = decltype(loads)::value;
     constexpr int kReads = TM + TN, kEach = (kReads + TM - 3) / (TM - 2), kLoadEach = 2 * kLoads / TM;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -481,125 +516,160 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
       x = next_step(buf);
     else if (t + 2 < n)
       fetch(t0 + t + 2);
-    work.template operator()<0, false>(buf, x);
+    work(First{}, std::false_type{}, buf, x);
     // Step t is in registers and step t + 1 in LDS, for every wave: step t's
     // buffer is free.
     if constexpr (ALIGNED) wait_loads<0>();
     barrier_lds();
-    work.template operator()<1, ALIGNED>(buf ^ 1, x);  // (after the last step: reads what is there, not used)
+    work(Second{}, std::bool_constant<ALIGNED>{}, buf ^ 1, x);  // (after the last step: reads what is there, not used)
     if constexpr (!ALIGNED)
       if (t + 2 < n) put(buf);
     asm volatile("" ::: "memory");  // the reads stay in this iteration
   }
   if constexpr (ALIGNED) wait_loads<0>();
 
-  // lane: row m of piece i, four columns from n of piece j
+  // Inside the matrices two neighbouring pieces are exchanged between the lanes so
+  // that each holds eight consecutive columns: 16-byte accesses (bf16).  At an edge a
+  // lane writes its four columns of a piece one by one.
   const int64_t mrow = m0 + wm * TM * 16 + (lane & 15);
-  const int nq = 4 * (lane >> 4);
+  const int64_t nwave = n0 + wn * (GU ? kHalf : TN * 16);
+  const int n4 = 4 * (lane >> 4), n8 = 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);
+  const bool inside = m0 + BM <= Mo && n0 + (GU ? BN / 2 : BN) <= No;
+  constexpr int kPairs = (GU ? TN / 2 : TN) / 2;
   if constexpr (MODE == kGateUp) {
     T *h = (T *)g.out[0], *su = (T *)g.out[1], *sv = (T *)g.out[2];
     const bool keep = su != nullptr;
+    if (inside) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
+          float u[8], v[8], x[8];
+          eight_columns(acc[i][2 * q], acc[i][2 * q + 1], u);
+          eight_columns(acc[i][TN / 2 + 2 * q], acc[i][TN / 2 + 2 * q + 1], v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = gate_act<T>(u[e], g.act) * v[e];
+          store8(h + at, x);
+          if (keep) {
+            store8(su + at, u);
+            store8(sv + at, v);
+          }
+        }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t m = mrow + i * 16;
       if (m >= Mo) continue;
 #pragma unroll
       for (int j = 0; j < TN / 2; ++j) {
-        const int64_t n = n0 + wn * 32 + j * 16 + nq, at = m * No + n;
-        const f32x4 u = acc[i][j], v = acc[i][j + TN / 2];
-        f32x4 x;
+        const int64_t n = nwave + j * 16 + n4, at = m * No + n;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = gate_act(u[e], g.act) * v[e];
-        if (n + 4 <= No) {
-          store4(h + at, x);
-          if (keep) {
-            store4(su + at, u);
-            store4(sv + at, v);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < No) {
-              h[at + e] = (T)x[e];
-              if (keep) {
-                su[at + e] = (T)u[e];
-                sv[at + e] = (T)v[e];
-              }
+        for (int e = 0; e < 4; ++e)
+          if (n + e < No) {
+            const float u = acc[i][j][e], v = acc[i][j + TN / 2][e];
+            h[at + e] = (T)(gate_act<T>(u, g.act) * v);
+            if (keep) {
+              su[at + e] = (T)u;
+              sv[at + e] = (T)v;
             }
-        }
+          }
       }
     }
   } else if constexpr (MODE == kHiddenGrad) {
     const T *pu = (const T *)g.u, *pv = (const T *)g.v;
     T *du = (T *)g.out[0], *dv = (T *)g.out[1], *h = (T *)g.out[2];
+    if (inside) {
+      // u and v of the next row of pieces travel while this one is worked on
+      Eight<T> nu[2][kPairs], nv[2][kPairs];
+      auto ask = [&](int i) {
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
+          nu[i & 1][q] = load8(pu + at);
+          nv[i & 1][q] = load8(pv + at);
+        }
+      };
+      ask(0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (i + 1 < TM) ask(i + 1);
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
+          float d[8], u[8], v[8], xu[8], xv[8], xh[8];
+          eight_columns(acc[i][2 * q], acc[i][2 * q + 1], d);
+          nu[i & 1][q].get(u);
+          nv[i & 1][q].get(v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float a, da;
+            gate_act_grad<T>(u[e], g.act, a, da);
+            xu[e] = d[e] * v[e] * da;
+            xv[e] = d[e] * a;
+            xh[e] = a * v[e];
+          }
+          store8(du + at, xu);
+          store8(dv + at, xv);
+          store8(h + at, xh);
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t m = mrow + i * 16;
       if (m >= Mo) continue;
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int64_t n = n0 + wn * TN * 16 + j * 16 + nq, at = m * No + n;
-        const f32x4 d = acc[i][j];
-        f32x4 u, v, xu, xv, xh;
-        if (n + 4 <= No) {
-          u = load4(pu + at);
-          v = load4(pv + at);
-        } else {
+        const int64_t n = nwave + j * 16 + n4, at = m * No + n;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            u[e] = n + e < No ? load1(pu + at + e) : 0.0f;
-            v[e] = n + e < No ? load1(pv + at + e) : 0.0f;
+        for (int e = 0; e < 4; ++e)
+          if (n + e < No) {
+            const float d = acc[i][j][e], u = load1(pu + at + e), v = load1(pv + at + e);
+            float a, da;
+            gate_act_grad<T>(u, g.act, a, da);
+            du[at + e] = (T)(d * v * da);
+            dv[at + e] = (T)(d * a);
+            h[at + e] = (T)(a * v);
           }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float a, da;
-          gate_act_grad(u[e], g.act, a, da);
-          xu[e] = d[e] * v[e] * da;
-          xv[e] = d[e] * a;
-          xh[e] = a * v[e];
-        }
-        if (n + 4 <= No) {
-          store4(du + at, xu);
-          store4(dv + at, xv);
-          store4(h + at, xh);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < No) {
-              du[at + e] = (T)xu[e];
-              dv[at + e] = (T)xv[e];
-              h[at + e] = (T)xh[e];
-            }
-        }
       }
     }
   } else {
     float *part = nullptr;
     if constexpr (MODE == kDown || MODE == kInputGrad)
       if (g.splits > 1) part = g.partial + (int64_t)prob * Mo * No;
+    if (inside) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
+          float x[8];
+          eight_columns(acc[i][2 * q], acc[i][2 * q + 1], x);
+          if (part)
+            store8(part + at, x);
+          else
+            store8(out + at, x);
+        }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t m = mrow + i * 16;
       if (m >= Mo) continue;
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int64_t n = n0 + wn * TN * 16 + j * 16 + nq, at = m * No + n;
-        const f32x4 x = acc[i][j];
-        if (part) {
-          if (n + 4 <= No)
-            store4(part + at, x);
-          else
+        const int64_t n = nwave + j * 16 + n4, at = m * No + n;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (n + e < No) part[at + e] = x[e];
-        } else if (n + 4 <= No) {
-          store4(out + at, x);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (n + e < No) out[at + e] = (T)x[e];
-        }
+        for (int e = 0; e < 4; ++e)
+          if (n + e < No) {
+            if (part)
+              part[at + e] = acc[i][j][e];
+            else
+              out[at + e] = (T)acc[i][j][e];
+          }
       }
     }
   }
