@@ -23,7 +23,7 @@ struct TileArgs {
   float *partial;           // [splits][M][N], where the sum is split
   int64_t M, N, K;          // output rows and columns (kWeightGrad: of the first two matrices), length of the sum
   int64_t task_stride;      // elements from one task's gradient row to the next
-  int tiles_m, tiles_n, splits, act;
+  int tiles_m, tiles_n, problems, splits, act;
   int64_t rows[kMaxK + 1];  // kWeightGrad: the tasks' rows
 };
 

@@ -264,270 +264,12 @@ __device__ __forceinline__ void tile_of(int id, int tm, int tn, int &m, int &n) 
   n = (id % per) / rows;
 }
 
-template <typename T, Mode MODE, int BM, int BN, int WM, int WN, bool ALIGNED>
-__global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g) {
-  constexpr int kWaves = WM * WN;
-  constexpr bool AKC = MODE != kWeightGrad;
-  constexpr bool BKC = MODE == kGateUp || MODE == kDown;
+// What becomes of a wave's sums.
+template <typename T, Mode MODE, int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)[BM / WM / 16][BN / WN / 16], int prob,
+                                           int64_t m0, int64_t n0, int64_t Mo, int64_t No, int wm, int wn, int lane) {
   constexpr bool GU = MODE == kGateUp;
-  using SA = Stage<T, BM, AKC, kWaves>;
-  using SB = Stage<T, BN, BKC, kWaves>;
-  constexpr int BK = SA::kBK, ES = sizeof(T);
-  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 pieces of a wave's tile
-  constexpr int kStep = SA::kBytes + SB::kBytes;
-  // a wave holds kHalf columns of the gate and the same kHalf of the up product
-  constexpr int kHalf = GU ? BN / WN / 2 : 0;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStep];
-
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-
-  // this workgroup's problem and tile
-  const int tiles = g.tiles_m * g.tiles_n;
-  int id = xcd_order(blockIdx.x, gridDim.x);
-  const int prob = id / tiles;
-  id -= prob * tiles;
-  Source<T> a[2] = {}, b[2] = {};
-  int segs = 1, tm = g.tiles_m, tn = g.tiles_n;
-  int64_t Mo = g.M, No = g.N, K = g.K;
-  T *out = (T *)g.out[0];
-  if constexpr (MODE == kWeightGrad) {
-    // problem: (task, matrix); the sum runs over the task's rows
-    const int task = prob / 3, mat = prob % 3;
-    const int64_t r0 = g.rows[task], r1 = g.rows[task + 1];
-    if (mat == 2) {  // [D][F] = dy^T h: the other two are [F][D]
-      const int64_t s = Mo;
-      Mo = No;
-      No = s;
-      tm = g.tiles_n;
-      tn = g.tiles_m;
-    }
-    K = r1 - r0;
-    a[0] = {(const T *)g.a[mat] + r0 * Mo, Mo, K};
-    b[0] = {(const T *)g.b[mat] + r0 * No, No, K};
-    out = (T *)g.out[mat] + task * g.task_stride;
-  } else {
-    a[0] = {(const T *)g.a[0], K, Mo};
-    b[0] = BKC ? Source<T>{(const T *)g.b[0], K, No} : Source<T>{(const T *)g.b[0], No, K};
-    if constexpr (MODE == kGateUp) b[1] = {(const T *)g.b[1], K, No};
-    if constexpr (MODE == kInputGrad) {
-      segs = 2;
-      a[1] = {(const T *)g.a[1], K, Mo};
-      b[1] = {(const T *)g.b[1], No, K};
-    }
-  }
-  int im, in;
-  tile_of(id, tm, tn, im, in);
-  const int64_t m0 = (int64_t)im * BM, n0 = (int64_t)in * (GU ? BN / 2 : BN);
-
-  // the steps of this workgroup: all of them, or its share of a split sum
-  const int steps_seg = (int)((K + BK - 1) / BK);
-  int t0 = 0, t1 = steps_seg * segs;
-  if constexpr (MODE == kDown || MODE == kInputGrad) {
-    if (g.splits > 1) {
-      const int per = (t1 + g.splits - 1) / g.splits;
-      t0 = prob * per < t1 ? prob * per : t1;
-      t1 = t0 + per < t1 ? t0 + per : t1;
-    }
-  }
-
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(BKMOO_LDS unsigned char *)lds;
-  uint32_t aoff[SA::kPer], boff[SB::kPer];
-  SA::template offsets<0>(wave, lane, a[0].ld, aoff);
-  SB::template offsets<kHalf>(wave, lane, b[0].ld, boff);
-
-  // Where the next step to load starts, and the bytes from there to its matrix's
-  // end (ALIGNED); none after the last step, so that its loads bring zeros.
-  struct Next {
-    const char *a, *b, *b2;
-    int64_t abytes, bbytes;
-    int left, t;  // of the segment's sum; step
-  } nx;
-  const int64_t astep = AKC ? 128 : (int64_t)BK * a[0].ld * ES, bstep = BKC ? 128 : (int64_t)BK * b[0].ld * ES;
-  auto start_at = [&](int t) {
-    const int seg = MODE == kInputGrad && t >= steps_seg ? 1 : 0;
-    const int64_t k0 = (int64_t)(t - seg * steps_seg) * BK;
-    const Source<T> &A = seg ? a[1] : a[0];
-    const Source<T> &B = seg ? b[1] : b[0];
-    const int64_t ea = AKC ? m0 * A.ld + k0 : k0 * A.ld + m0;
-    const int64_t eb = BKC ? n0 * B.ld + k0 : k0 * B.ld + n0;
-    nx.a = (const char *)(A.p + ea);
-    nx.b = (const char *)(B.p + eb);
-    nx.b2 = GU ? (const char *)(b[1].p + eb) : nx.b;
-    nx.abytes = (A.rows * A.ld - ea) * ES;
-    nx.bbytes = (B.rows * B.ld - eb) * ES;
-    nx.left = (int)(K - k0);
-    nx.t = t;
-  };
-  struct Step {
-    i32x4 a, b, b2;
-    uint32_t la, lb;
-    int left;
-  };
-  auto next_step = [&](int buf) {
-    Step x;
-    x.a = make_desc(nx.a, nx.abytes);
-    x.b = make_desc(nx.b, nx.bbytes);
-    x.b2 = GU ? make_desc(nx.b2, nx.bbytes) : x.b;
-    x.la = lds0 + buf * kStep + wave * SA::kPer * 1024;
-    x.lb = lds0 + buf * kStep + SA::kBytes + wave * SB::kPer * 1024;
-    x.left = nx.left;
-    nx.a += astep;
-    nx.b += bstep;
-    nx.b2 += bstep;
-    nx.abytes -= astep;
-    nx.bbytes -= bstep;
-    nx.left -= BK;
-    ++nx.t;
-    if (nx.t >= t1)
-      nx.abytes = nx.bbytes = 0;
-    else if (MODE == kInputGrad && nx.t == steps_seg)
-      start_at(nx.t);
-    return x;
-  };
-  constexpr int kLoads = SA::kPer + SB::kPer;
-  auto piece = [&](const Step &x, int i) {
-    if (i < SA::kPer) {
-      uint32_t off = aoff[i];
-      if (AKC && x.left < BK) {
-        int row, chunk;
-        SA::place(wave * SA::kPer + i, lane, row, chunk);
-        if (chunk * (16 / ES) >= x.left) off = kNowhere;
-      }
-      load_to_lds(x.la + i * 1024, x.a, off);
-    } else {
-      const int q = i - SA::kPer;
-      uint32_t off = boff[q];
-      if (BKC && x.left < BK) {
-        int row, chunk;
-        SB::place(wave * SB::kPer + q, lane, row, chunk);
-        if (chunk * (16 / ES) >= x.left) off = kNowhere;
-      }
-      load_to_lds(x.lb + q * 1024, SB::template second<kHalf>(wave, q) ? x.b2 : x.b, off);
-    }
-  };
-
-  // the same through registers, element by element where a chunk crosses an end
-  u32x4 ra[ALIGNED ? 1 : SA::kPer], rb[ALIGNED ? 1 : SB::kPer];
-  auto fetch = [&](int t) {
-    const int seg = MODE == kInputGrad && t >= steps_seg ? 1 : 0;
-    const int64_t k0 = (int64_t)(t - seg * steps_seg) * BK;
-    const Source<T> &A = seg ? a[1] : a[0];
-    if constexpr (!ALIGNED) {
-#pragma unroll
-      for (int i = 0; i < SA::kPer; ++i) {
-        int row, chunk;
-        SA::place(wave * SA::kPer + i, lane, row, chunk);
-        const int64_t r = (AKC ? m0 : k0) + row, c = (AKC ? k0 : m0) + chunk * (16 / ES);
-        ra[i] = r < A.rows ? guarded_chunk(A.p + r * A.ld, c, A.ld) : u32x4{0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int i = 0; i < SB::kPer; ++i) {
-        int row, chunk;
-        SB::place(wave * SB::kPer + i, lane, row, chunk);
-        const Source<T> &B = (GU ? SB::template second<kHalf>(wave, i) : seg != 0) ? b[1] : b[0];
-        if constexpr (GU) row = row / (2 * kHalf) * kHalf + row % kHalf;
-        const int64_t r = (BKC ? n0 : k0) + row, c = (BKC ? k0 : n0) + chunk * (16 / ES);
-        rb[i] = r < B.rows ? guarded_chunk(B.p + r * B.ld, c, B.ld) : u32x4{0, 0, 0, 0};
-      }
-    }
-  };
-  auto put = [&](int slot) {
-    if constexpr (!ALIGNED) {
-      const uint32_t la = lds0 + slot * kStep + wave * SA::kPer * 1024 + lane * 16;
-      const uint32_t lb = lds0 + slot * kStep + SA::kBytes + wave * SB::kPer * 1024 + lane * 16;
-#pragma unroll
-      for (int i = 0; i < SA::kPer; ++i) *(BKMOO_LDS u32x4 *)(uintptr_t)(la + i * 1024) = ra[i];
-#pragma unroll
-      for (int i = 0; i < SB::kPer; ++i) *(BKMOO_LDS u32x4 *)(uintptr_t)(lb + i * 1024) = rb[i];
-    }
-  };
-
-  f32x4 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-
-  const int wm = wave / WN, wn = wave % WN;
-  const Reader<T, BM, AKC> reada(wm * TM * 16, lane);
-  const Reader<T, BN, BKC> readb(wn * TN * 16, lane);
-
-  using First = std::integral_constant<int, 0>;
-  using Second = std::integral_constant<int, 1>;
-  // Fragments of both halves of a step: one is multiplied while the other is read.
-  Frag<T> fa[2][TM], fb[2][TN];
-  auto read = [&](int half, int buf, int i) {
-    const uint32_t la = lds0 + buf * kStep;
-    if (i < TN)
-      fb[half][i] = readb.read(la + SA::kBytes, half, i);
-    else
-      fa[half][i - TN] = reada.read(la, half, i - TN);
-  };
-  // The products of a half, row by row of pieces, with the reads of the other half (of
-  // the step in LDS buffer `buf`) and, LOAD, the loads of a step in between: none holds up
-  // another, and every read has arrived when the half ends.
-  auto work = [&](auto half, auto loads, int buf, const Step &x) {
-    constexpr int HALF = decltype(half)::value;
-    constexpr bool LOAD = decltype(loads)::value;
-    constexpr int kReads = TM + TN, kEach = (kReads + TM - 3) / (TM - 2), kLoadEach = 2 * kLoads / TM;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-#pragma unroll
-      for (int q = i * kEach; q < (i + 1) * kEach; ++q)
-        if (q < kReads) read(HALF ^ 1, buf, q);
-      if constexpr (LOAD)
-#pragma unroll
-        for (int q = i * kLoadEach; q < (i + 1) * kLoadEach; ++q)
-          if (q < kLoads) piece(x, q);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  const int n = t1 - t0;
-  Step x = {};
-  if (n > 0) {
-    if constexpr (ALIGNED) {
-      start_at(t0);
-      x = next_step(0);
-#pragma unroll
-      for (int q = 0; q < kLoads; ++q) piece(x, q);
-      x = next_step(1);
-#pragma unroll
-      for (int q = 0; q < kLoads; ++q) piece(x, q);
-      wait_loads<kLoads>();
-    } else {
-      fetch(t0);
-      put(0);
-      if (n > 1) {
-        fetch(t0 + 1);
-        put(1);
-      }
-    }
-    barrier_lds();
-#pragma unroll
-    for (int i = 0; i < TM + TN; ++i) read(0, 0, i);
-  }
-  for (int t = 0; t < n; ++t) {
-    const int buf = t & 1;
-    if constexpr (ALIGNED)
-      x = next_step(buf);
-    else if (t + 2 < n)
-      fetch(t0 + t + 2);
-    work(First{}, std::false_type{}, buf, x);
-    // Step t is in registers and step t + 1 in LDS, for every wave: step t's
-    // buffer is free.
-    if constexpr (ALIGNED) wait_loads<0>();
-    barrier_lds();
-    work(Second{}, std::bool_constant<ALIGNED>{}, buf ^ 1, x);  // (after the last step: reads what is there, not used)
-    if constexpr (!ALIGNED)
-      if (t + 2 < n) put(buf);
-    asm volatile("" ::: "memory");  // the reads stay in this iteration
-  }
-  if constexpr (ALIGNED) wait_loads<0>();
-
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16, kHalf = GU ? BN / WN / 2 : 0;
   // Inside the matrices two neighbouring pieces are exchanged between the lanes so
   // that each holds eight consecutive columns: 16-byte accesses (bf16).  At an edge a
   // lane writes its four columns of a piece one by one.
@@ -637,6 +379,7 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
       }
     }
   } else {
+    T *out = MODE == kWeightGrad ? (T *)g.out[prob % 3] + (prob / 3) * g.task_stride : (T *)g.out[0];
     float *part = nullptr;
     if constexpr (MODE == kDown || MODE == kInputGrad)
       if (g.splits > 1) part = g.partial + (int64_t)prob * Mo * No;
@@ -673,6 +416,324 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_tile_kernel(const TileArgs g
       }
     }
   }
+}
+
+// The epilogue's stores that a wave has certainly queued after a tile inside the
+// matrices (at most what the counter holds).
+template <typename T, Mode MODE, int TM, int TN>
+constexpr int kTileStores = [] {
+  const int pairs = TM * (MODE == kGateUp ? TN / 2 : TN) / 2 * (sizeof(T) == 4 ? 2 : 1);
+  const int n = MODE == kHiddenGrad ? 3 * pairs : pairs;
+  return n < 63 ? n : 63;
+}();
+
+template <typename T, Mode MODE, int BM, int BN, int WM, int WN, bool ALIGNED>
+__global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArgs g) {
+  constexpr int kWaves = WM * WN;
+  constexpr bool AKC = MODE != kWeightGrad;
+  constexpr bool BKC = MODE == kGateUp || MODE == kDown;
+  constexpr bool GU = MODE == kGateUp;
+  using SA = Stage<T, BM, AKC, kWaves>;
+  using SB = Stage<T, BN, BKC, kWaves>;
+  constexpr int BK = SA::kBK, ES = sizeof(T);
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;  // 16 x 16 pieces of a wave's tile
+  constexpr int kStep = SA::kBytes + SB::kBytes;
+  // a wave holds kHalf columns of the gate and the same kHalf of the up product
+  constexpr int kHalf = GU ? BN / WN / 2 : 0;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStep];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(BKMOO_LDS unsigned char *)lds;
+  const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.problems;
+  constexpr bool kMany = MODE != kHiddenGrad;  // tiles a workgroup (at least one: the grid is no larger)
+
+  // A tile: its problem, its place, and its steps t0 to t1 (all, or its share of a
+  // split sum).
+  struct Tile {
+    int prob, steps_seg, t0, t1;
+    int64_t m0, n0, M, N, K;
+  };
+  auto tile = [&](int round) {
+    const int first = round * (int)gridDim.x, here = total - first < (int)gridDim.x ? total - first : (int)gridDim.x;
+    int id = first + xcd_order(blockIdx.x, here);
+    Tile x;
+    x.prob = id / tiles;
+    id -= x.prob * tiles;
+    x.M = g.M;
+    x.N = g.N;
+    x.K = g.K;
+    int tm = g.tiles_m, tn = g.tiles_n, im, in;
+    if constexpr (MODE == kWeightGrad) {
+      // problem: (task, matrix); the sum runs over the task's rows
+      const int task = x.prob / 3;
+      if (x.prob % 3 == 2) {  // [D][F] = dy^T h: the other two are [F][D]
+        x.M = g.N;
+        x.N = g.M;
+        tm = g.tiles_n;
+        tn = g.tiles_m;
+      }
+      x.K = g.rows[task + 1] - g.rows[task];
+    }
+    tile_of(id, tm, tn, im, in);
+    x.m0 = (int64_t)im * BM;
+    x.n0 = (int64_t)in * (GU ? BN / 2 : BN);
+    x.steps_seg = (int)((x.K + BK - 1) / BK);
+    x.t0 = 0;
+    x.t1 = x.steps_seg * (MODE == kInputGrad ? 2 : 1);
+    if constexpr (MODE == kDown || MODE == kInputGrad) {
+      if (g.splits > 1) {
+        const int per = (x.t1 + g.splits - 1) / g.splits;
+        x.t0 = x.prob * per < x.t1 ? x.prob * per : x.t1;
+        x.t1 = x.t0 + per < x.t1 ? x.t0 + per : x.t1;
+      }
+    }
+    return x;
+  };
+  // Its operands: the matrix (of the segment of the sum that step t is in) and its rows.
+  auto source_a = [&](const Tile &x, int seg) {
+    if constexpr (MODE == kWeightGrad) return Source<T>{(const T *)g.a[x.prob % 3] + g.rows[x.prob / 3] * x.M, x.M, x.K};
+    return Source<T>{(const T *)(seg ? g.a[1] : g.a[0]), x.K, x.M};
+  };
+  auto source_b = [&](const Tile &x, int seg) {
+    if constexpr (MODE == kWeightGrad) return Source<T>{(const T *)g.b[x.prob % 3] + g.rows[x.prob / 3] * x.N, x.N, x.K};
+    const T *p = (const T *)(seg ? g.b[1] : g.b[0]);
+    return BKC ? Source<T>{p, x.K, x.N} : Source<T>{p, x.N, x.K};
+  };
+
+  // The stream of steps to load (ALIGNED): those of all this workgroup's tiles, one after
+  // another, so that the next tile's first steps travel while a tile ends.  Where the
+  // next one starts, and the bytes from there to its matrix's end; none after the last
+  // step: its loads bring zeros.
+  struct Next {
+    const char *a, *b, *b2;
+    int64_t abytes, bbytes, astep, bstep;
+    int left, t, seg_end, t1, round;  // left: of the segment's sum
+  } nx = {};
+  uint32_t aoff[SA::kPer], boff[SB::kPer];
+  auto start_at = [&](const Tile &x, int t) {
+    const int seg = MODE == kInputGrad && t >= x.steps_seg ? 1 : 0;
+    const int64_t k0 = (int64_t)(t - seg * x.steps_seg) * BK;
+    const Source<T> A = source_a(x, seg), B = source_b(x, seg);
+    const int64_t ea = AKC ? x.m0 * A.ld + k0 : k0 * A.ld + x.m0;
+    const int64_t eb = BKC ? x.n0 * B.ld + k0 : k0 * B.ld + x.n0;
+    nx.a = (const char *)(A.p + ea);
+    nx.b = (const char *)(B.p + eb);
+    nx.b2 = GU ? (const char *)((const T *)g.b[1] + eb) : nx.b;
+    nx.abytes = (A.rows * A.ld - ea) * ES;
+    nx.bbytes = (B.rows * B.ld - eb) * ES;
+    nx.astep = AKC ? 128 : BK * A.ld * ES;
+    nx.bstep = BKC ? 128 : BK * B.ld * ES;
+    nx.left = (int)(x.K - k0);
+    nx.t = t;
+    nx.seg_end = MODE == kInputGrad && seg == 0 ? x.steps_seg : x.t1;
+    nx.t1 = x.t1;
+  };
+  auto start_tile = [&](int round) {
+    for (; round == 0 || (kMany && round * (int)gridDim.x + (int)blockIdx.x < total); ++round) {
+      const Tile x = tile(round);
+      if (x.t0 >= x.t1) continue;
+      if (MODE == kWeightGrad || nx.t1 == 0) {
+        SA::template offsets<0>(wave, lane, source_a(x, 0).ld, aoff);
+        SB::template offsets<kHalf>(wave, lane, source_b(x, 0).ld, boff);
+      }
+      start_at(x, x.t0);
+      nx.round = round;
+      return;
+    }
+    nx.abytes = nx.bbytes = nx.astep = nx.bstep = 0;
+    nx.seg_end = nx.t1 = 0x7fffffff;
+    nx.t = 0;
+  };
+  struct Step {
+    i32x4 a, b, b2;
+    uint32_t la, lb;
+    int left;
+  };
+  auto next_step = [&](int buf) {
+    Step x;
+    x.a = make_desc(nx.a, nx.abytes);
+    x.b = make_desc(nx.b, nx.bbytes);
+    x.b2 = GU ? make_desc(nx.b2, nx.bbytes) : x.b;
+    x.la = lds0 + buf * kStep + wave * SA::kPer * 1024;
+    x.lb = lds0 + buf * kStep + SA::kBytes + wave * SB::kPer * 1024;
+    x.left = nx.left;
+    nx.a += nx.astep;
+    nx.b += nx.bstep;
+    nx.b2 += nx.bstep;
+    nx.abytes -= nx.astep;
+    nx.bbytes -= nx.bstep;
+    nx.left -= BK;
+    ++nx.t;
+    return x;
+  };
+  // Behind the loads of a step: the offsets may be another matrix's from here on.
+  auto move_on = [&]() {
+    if (nx.t < nx.seg_end) return;
+    if (MODE == kInputGrad && nx.t < nx.t1)
+      start_at(tile(nx.round), nx.t);
+    else
+      start_tile(nx.round + 1);
+  };
+  constexpr int kLoads = SA::kPer + SB::kPer;
+  auto piece = [&](const Step &x, int i) {
+    if (i < SA::kPer) {
+      uint32_t off = aoff[i];
+      if (AKC && x.left < BK) {
+        int row, chunk;
+        SA::place(wave * SA::kPer + i, lane, row, chunk);
+        if (chunk * (16 / ES) >= x.left) off = kNowhere;
+      }
+      load_to_lds(x.la + i * 1024, x.a, off);
+    } else {
+      const int q = i - SA::kPer;
+      uint32_t off = boff[q];
+      if (BKC && x.left < BK) {
+        int row, chunk;
+        SB::place(wave * SB::kPer + q, lane, row, chunk);
+        if (chunk * (16 / ES) >= x.left) off = kNowhere;
+      }
+      load_to_lds(x.lb + q * 1024, SB::template second<kHalf>(wave, q) ? x.b2 : x.b, off);
+    }
+  };
+
+  // Steps through registers, element by element where a chunk crosses an end (!ALIGNED).
+  u32x4 ra[ALIGNED ? 1 : SA::kPer], rb[ALIGNED ? 1 : SB::kPer];
+  auto fetch = [&](const Tile &x, int t) {
+    if constexpr (!ALIGNED) {
+      const int seg = MODE == kInputGrad && t >= x.steps_seg ? 1 : 0;
+      const int64_t k0 = (int64_t)(t - seg * x.steps_seg) * BK;
+      const Source<T> A = source_a(x, seg), B = source_b(x, seg);
+#pragma unroll
+      for (int i = 0; i < SA::kPer; ++i) {
+        int row, chunk;
+        SA::place(wave * SA::kPer + i, lane, row, chunk);
+        const int64_t r = (AKC ? x.m0 : k0) + row, c = (AKC ? k0 : x.m0) + chunk * (16 / ES);
+        ra[i] = r < A.rows ? guarded_chunk(A.p + r * A.ld, c, A.ld) : u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int i = 0; i < SB::kPer; ++i) {
+        int row, chunk;
+        SB::place(wave * SB::kPer + i, lane, row, chunk);
+        const T *p = GU && SB::template second<kHalf>(wave, i) ? (const T *)g.b[1] : B.p;
+        if constexpr (GU) row = row / (2 * kHalf) * kHalf + row % kHalf;
+        const int64_t r = (BKC ? x.n0 : k0) + row, c = (BKC ? k0 : x.n0) + chunk * (16 / ES);
+        rb[i] = r < B.rows ? guarded_chunk(p + r * B.ld, c, B.ld) : u32x4{0, 0, 0, 0};
+      }
+    }
+  };
+  auto put = [&](int buf) {
+    if constexpr (!ALIGNED) {
+      const uint32_t la = lds0 + buf * kStep + wave * SA::kPer * 1024 + lane * 16;
+      const uint32_t lb = lds0 + buf * kStep + SA::kBytes + wave * SB::kPer * 1024 + lane * 16;
+#pragma unroll
+      for (int i = 0; i < SA::kPer; ++i) *(BKMOO_LDS u32x4 *)(uintptr_t)(la + i * 1024) = ra[i];
+#pragma unroll
+      for (int i = 0; i < SB::kPer; ++i) *(BKMOO_LDS u32x4 *)(uintptr_t)(lb + i * 1024) = rb[i];
+    }
+  };
+
+  f32x4 acc[TM][TN];
+  const int wm = wave / WN, wn = wave % WN;
+  const Reader<T, BM, AKC> reada(wm * TM * 16, lane);
+  const Reader<T, BN, BKC> readb(wn * TN * 16, lane);
+
+  // Fragments of both halves of a step: one is multiplied while the other is read.
+  Frag<T> fa[2][TM], fb[2][TN];
+  auto read = [&](int half, int buf, int i) {
+    const uint32_t la = lds0 + buf * kStep;
+    if (i < TN)
+      fb[half][i] = readb.read(la + SA::kBytes, half, i);
+    else
+      fa[half][i - TN] = reada.read(la, half, i - TN);
+  };
+  // The products of a half, row by row of pieces, with the reads of the other half (of
+  // the step in LDS buffer `buf`) and, LOAD, the loads of a step in between: none holds up
+  // another, and every read has arrived when the half ends.
+  auto work = [&](auto half, auto loads, int buf, const Step &x) {
+    constexpr int HALF = decltype(half)::value;
+    constexpr bool LOAD = decltype(loads)::value;
+    constexpr int kReads = TM + TN, kEach = (kReads + TM - 3) / (TM - 2), kLoadEach = 2 * kLoads / TM;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+#pragma unroll
+      for (int q = i * kEach; q < (i + 1) * kEach; ++q)
+        if (q < kReads) read(HALF ^ 1, buf, q);
+      if constexpr (LOAD)
+#pragma unroll
+        for (int q = i * kLoadEach; q < (i + 1) * kLoadEach; ++q)
+          if (q < kLoads) piece(x, q);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  using First = std::integral_constant<int, 0>;
+  using Second = std::integral_constant<int, 1>;
+  using Loads = std::bool_constant<ALIGNED>;
+
+  Step x = {};
+  if constexpr (ALIGNED) {
+    start_tile(0);
+    for (int i = 0; i < 2; ++i) {
+      x = next_step(i);
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) piece(x, q);
+      move_on();
+    }
+    wait_loads<kLoads>();
+    barrier_lds();
+  }
+  int buf = 0;
+  bool stored = false;  // since the last wait: a tile inside the matrices
+  for (int round = 0; round == 0 || (kMany && round * (int)gridDim.x + (int)blockIdx.x < total); ++round) {
+    const Tile z = tile(round);
+    const int n = z.t1 - z.t0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    if constexpr (!ALIGNED) {
+      barrier_lds();
+      buf = 0;
+      for (int i = 0; i < 2 && i < n; ++i) {
+        fetch(z, z.t0 + i);
+        put(i);
+      }
+      barrier_lds();
+    }
+    if (n > 0) {
+#pragma unroll
+      for (int i = 0; i < TM + TN; ++i) read(0, buf, i);
+    }
+    for (int t = 0; t < n; ++t, buf ^= 1) {
+      if constexpr (ALIGNED)
+        x = next_step(buf);
+      else if (t + 2 < n)
+        fetch(z, z.t0 + t + 2);
+      work(First{}, std::false_type{}, buf, x);
+      // Step t is in registers and step t + 1 in LDS, for every wave: step t's
+      // buffer is free.  (The stores of the tile before need not have ended: they were
+      // queued behind the loads waited for.)
+      if constexpr (ALIGNED) {
+        if (stored)
+          wait_loads<kTileStores<T, MODE, TM, TN>>();
+        else
+          wait_loads<0>();
+        stored = false;
+      }
+      barrier_lds();
+      work(Second{}, Loads{}, buf ^ 1, x);  // (after the last step: reads what is there)
+      if constexpr (ALIGNED)
+        move_on();
+      else if (t + 2 < n)
+        put(buf);
+      asm volatile("" ::: "memory");  // the reads stay in this iteration
+    }
+    stored = z.m0 + BM <= z.M && z.n0 + (GU ? BN / 2 : BN) <= z.N;
+    store_tile<T, MODE, BM, BN, WM, WN>(g, acc, z.prob, z.m0, z.n0, z.M, z.N, wm, wn, lane);
+  }
+  if constexpr (ALIGNED) wait_loads<0>();  // LDS is still being written
 }
 
 }  // namespace bkmoo

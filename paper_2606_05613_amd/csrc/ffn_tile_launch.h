@@ -12,17 +12,26 @@ hipError_t launch_mode(TileArgs g, int tasks, bool wide, hipStream_t s) {
   const int side = wide ? 256 : 128;
   g.tiles_m = (int)((rows + side - 1) / side);
   g.tiles_n = (int)((cols + side - 1) / side);
-  const int64_t probs = MODE == kWeightGrad ? 3 * tasks : g.splits > 1 ? g.splits : 1;
-  const int64_t n = (int64_t)g.tiles_m * g.tiles_n * probs;
+  g.problems = MODE == kWeightGrad ? 3 * tasks : g.splits > 1 ? g.splits : 1;
+  const int64_t n = (int64_t)g.tiles_m * g.tiles_n * g.problems;
   if (n == 0) return hipSuccess;
-  if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (n > 0x3fffffff) return hipErrorInvalidConfiguration;
+  // As many workgroups as the chip holds at once (one of 512 threads or two of 256 a CU), each
+  // with tiles to the end: a tile's first steps travel while the one before is stored
+  // (M=4096, D=2048, F=6144, us, a workgroup a tile / these: gate and up 178 / 167, down 114 /
+  // 95, weight gradients 324 / 301; 8192 x 4096 x 14336: 1772 / 1749, 857 / 852, 2564 / 2525).
+  // The hidden gradient's epilogue waits for loads of its own, which the next tile's would
+  // hold up: a workgroup a tile (963 / 1079).
+  const int64_t cus = MODE == kHiddenGrad ? n : device_cu_count();
   if constexpr (ALIGNED) {
     if (wide) {
-      ffn_tile_kernel<T, MODE, 256, 256, 2, 4, true><<<dim3((unsigned)n), dim3(512), 0, s>>>(g);
+      const unsigned grid = (unsigned)(n < cus ? n : cus);
+      ffn_tile_kernel<T, MODE, 256, 256, 2, 4, true><<<dim3(grid), dim3(512), 0, s>>>(g);
       return hipGetLastError();
     }
   }
-  ffn_tile_kernel<T, MODE, 128, 128, 2, 2, ALIGNED><<<dim3((unsigned)n), dim3(256), 0, s>>>(g);
+  const unsigned grid = (unsigned)(n < 2 * cus ? n : 2 * cus);
+  ffn_tile_kernel<T, MODE, 128, 128, 2, 2, ALIGNED><<<dim3(grid), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
 
