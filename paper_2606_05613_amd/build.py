@@ -42,7 +42,7 @@ ARCH = "gfx950"
 
 SOURCES = ["api.hip", "schedule.hip", "gram.hip", "solve.hip", "solve_exact.hip", "combine.hip",
            "hybrid.hip", "refill.hip", "conflicts.hip", "slices.hip",
-           "ffn.hip", "ffn_bf16.hip", "ffn_f32.hip", "norm.hip", "adamw.hip"]
+           "ffn.hip", "ffn_few.hip", "ffn_bf16.hip", "ffn_f32.hip", "norm.hip", "adamw.hip"]
 EXTRA = {"solve.hip": ["-ffp-contract=off"], "solve_exact.hip": ["-ffp-contract=off"],
          "hybrid.hip": ["-ffp-contract=off"], "refill.hip": ["-ffp-contract=off"],
          "conflicts.hip": ["-ffp-contract=off"], "adamw.hip": ["-ffp-contract=off"]}

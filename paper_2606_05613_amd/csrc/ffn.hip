@@ -133,6 +133,9 @@ extern "C" bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo
   char *ws = (char *)workspace;
   const int64_t v = 16 / (int64_t)es;
   const bool aligned = D % v == 0 && F % v == 0 && at16(x) && at16(w_gate) && at16(w_up) && at16(w_down);
+  if (M <= kFewRows)
+    return status_of(launch_ffn_few(dt, x, w_gate, w_up, w_down, ws + L.h, y, gate_out, up_out, M, D, F,
+                                    act == BKMOO_SILU ? kSilu : kGelu, aligned, stream));
   TileArgs g = {};
   g.a[0] = x;
   g.b[0] = w_gate;
