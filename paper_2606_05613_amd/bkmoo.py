@@ -452,9 +452,21 @@ def _ptr(t: Optional[torch.Tensor], shape, like: torch.Tensor, what: str):
     """Pointer of a contiguous tensor of `like`'s type and device; None stays None."""
     if t is None:
         return None
-    if t.dtype != like.dtype or t.shape != shape or not t.is_contiguous() or t.device != like.device:
-        raise ValueError(f"{what} must be a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
-    return t.data_ptr()
+    if t.dtype is like.dtype and t.shape == shape and t.is_contiguous() and t.get_device() == like.get_device():
+        return t.data_ptr()
+    raise ValueError(f"{what} must be a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+
+
+def _run(fn, what: str, dev, *args):
+    """fn(*args, stream) with the inputs' device current."""
+    stream = torch.cuda.current_stream(dev.index).cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        st = fn(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, stream)
+    if st != 0:
+        _check(st, what)
 
 
 def _matrix(t: torch.Tensor, what: str):
@@ -516,8 +528,7 @@ def residual_norm_forward(resid: torch.Tensor, y: torch.Tensor, weight: torch.Te
     args = (_ptr(resid, shape, resid, "resid"), _ptr(y, shape, resid, "y"), _ptr(weight, vec, resid, "weight"),
             _ptr(post_weight, vec, resid, "post_weight"), _ptr(gate, vec, resid, "gate"), scale, eps,
             _ptr(resid_out, shape, resid, "resid_out"), _ptr(normed, shape, resid, "normed"))
-    with torch.cuda.device(dev):
-        _check(_lib.bkmoo_residual_norm_forward(M, D, dt, *args, _stream_ptr(dev)), "bkmoo_residual_norm_forward")
+    _run(_lib.bkmoo_residual_norm_forward, "bkmoo_residual_norm_forward", dev, M, D, dt, *args)
     return resid_out, normed
 
 
@@ -548,9 +559,8 @@ def residual_norm_backward(dresid_out: Optional[torch.Tensor], dnormed: torch.Te
             _ptr(resid_out, shape, like, "resid_out"), _ptr(y, shape, like, "y"), _ptr(weight, vec, like, "weight"),
             _ptr(post_weight, vec, like, "post_weight"), _ptr(gate, vec, like, "gate"), scale, eps,
             _ptr(dresid, shape, like, "dresid"), _ptr(dy, shape, like, "dy"), *ptrs, stride)
-    with torch.cuda.device(dev):
-        _check(_lib.bkmoo_residual_norm_backward(M, D, dt, K, rows, *args, ws.data_ptr(), ws.numel(),
-                                                 _stream_ptr(dev)), "bkmoo_residual_norm_backward")
+    _run(_lib.bkmoo_residual_norm_backward, "bkmoo_residual_norm_backward", dev, M, D, dt, K, rows, *args,
+         ws.data_ptr(), ws.numel())
     return dresid, dy
 
 
@@ -581,9 +591,7 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
     args = (_ptr(x, (M, D), x, "x"), _ptr(w_gate, (F, D), x, "w_gate"), _ptr(w_up, (F, D), x, "w_up"),
             _ptr(w_down, (D, F), x, "w_down"), _ptr(out, (M, D), x, "out"), _ptr(gate_out, (M, F), x, "gate_out"),
             _ptr(up_out, (M, F), x, "up_out"))
-    with torch.cuda.device(dev):
-        _check(_lib.bkmoo_ffn_forward(M, D, F, dt, ACTS[act], *args, ws.data_ptr(), ws.numel(), _stream_ptr(dev)),
-               "bkmoo_ffn_forward")
+    _run(_lib.bkmoo_ffn_forward, "bkmoo_ffn_forward", dev, M, D, F, dt, ACTS[act], *args, ws.data_ptr(), ws.numel())
     return out, gate_out, up_out
 
 
@@ -610,9 +618,8 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate_out: torch.Tensor, up_o
     args = (_ptr(dy, (M, D), x, "dy"), _ptr(x, (M, D), x, "x"), _ptr(gate_out, (M, F), x, "gate_out"),
             _ptr(up_out, (M, F), x, "up_out"), _ptr(w_gate, (F, D), x, "w_gate"), _ptr(w_up, (F, D), x, "w_up"),
             _ptr(w_down, (D, F), x, "w_down"), _ptr(dx, (M, D), x, "dx"), *ptrs, stride)
-    with torch.cuda.device(dev):
-        _check(_lib.bkmoo_ffn_backward(M, D, F, dt, ACTS[act], K, rows, *args, ws.data_ptr(), ws.numel(),
-                                       _stream_ptr(dev)), "bkmoo_ffn_backward")
+    _run(_lib.bkmoo_ffn_backward, "bkmoo_ffn_backward", dev, M, D, F, dt, ACTS[act], K, rows, *args, ws.data_ptr(),
+         ws.numel())
     return dx
 
 
@@ -667,7 +674,5 @@ def adamw(table: AdamwTable, grad: torch.Tensor, moment1: torch.Tensor, moment2:
             raise ValueError(f"grad_scale must be one float32 value on {dev}")
         gs = grad_scale.data_ptr()
     hp = _AdamwHparams(lr, beta1, beta2, eps, weight_decay, step, seed & 0xFFFFFFFF)
-    with torch.cuda.device(dev):
-        _check(_lib.bkmoo_adamw(len(table.params), table.array, table.dt, N, gp, _dt(grad), STATE_F8 if f8 else STATE_F32,
-                                m1, m2, sc, table.blocks if f8 else 0, mp, ctypes.byref(hp), gs, _stream_ptr(dev)),
-               "bkmoo_adamw")
+    _run(_lib.bkmoo_adamw, "bkmoo_adamw", dev, len(table.params), table.array, table.dt, N, gp, _dt(grad),
+         STATE_F8 if f8 else STATE_F32, m1, m2, sc, table.blocks if f8 else 0, mp, ctypes.byref(hp), gs)

@@ -15,16 +15,29 @@ __device__ __forceinline__ float load1(const float *p) { return *p; }
 __device__ __forceinline__ float load1(const __bf16 *p) { return (float)*p; }
 
 // The 16 bytes of a chunk that starts at element c of a row of `n` elements (any
-// alignment), zeros past the row's end.
+// alignment), zeros past the row's end: a chunk that crosses it is the row's last 16 bytes,
+// moved down.
 template <typename T>
 __device__ __forceinline__ u32x4 guarded_chunk(const T *row, int64_t c, int64_t n) {
   constexpr int V = 16 / sizeof(T);
-  if (c + V <= n) return *(const u32x4_any *)(row + c);
   union {
     u32x4 v;
+    uint64_t d[2];
     uint32_t w[4];
     uint16_t h[8];
   } x;
+  if (n >= V) {
+    const int64_t from = c + V <= n ? c : n - V;
+    x.v = *(const u32x4_any *)(row + from);
+    if (from != c) {
+      const int64_t over = c - from;
+      const int bits = over < V ? (int)over * (int)sizeof(T) * 8 : 128;
+      const uint64_t lo = x.d[0], hi = x.d[1];
+      x.d[0] = bits < 64 ? (lo >> bits) | (hi << 1 << (63 - bits)) : bits < 128 ? hi >> (bits - 64) : 0;
+      x.d[1] = bits < 64 ? hi >> bits : 0;
+    }
+    return x.v;
+  }
   x.v = u32x4{0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < V; ++e)
@@ -110,14 +123,24 @@ __device__ __forceinline__ void guarded_store(T *row, int64_t c, int64_t n, u32x
     *(u32x4_any *)(row + c) = v;
     return;
   }
-  union {
-    u32x4 v;
-    T e[V];
-  } x;
-  x.v = v;
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (c + e < n) row[c + e] = x.e[e];
+  if (c >= n) return;
+  // 8, 4 and 2 bytes, as the elements left make up
+  typedef uint64_t u64_any __attribute__((aligned(2)));
+  typedef uint32_t u32_any __attribute__((aligned(2)));
+  char *p = (char *)(row + c);
+  const int bytes = (int)(n - c) * (int)sizeof(T);
+  uint64_t d = (uint64_t)v.y << 32 | v.x;
+  if (bytes & 8) {
+    *(u64_any *)p = d;
+    p += 8;
+    d = (uint64_t)v.w << 32 | v.z;
+  }
+  if (bytes & 4) {
+    *(u32_any *)p = (uint32_t)d;
+    p += 4;
+    d >>= 32;
+  }
+  if (bytes & 2) *(uint16_t *)p = (uint16_t)d;
 }
 
 }  // namespace bkmoo

@@ -9,7 +9,9 @@
 // Everything is a sum over a row or a column of M x D elements that are read
 // once: memory-bound.  A row stays in registers as it was read (16-byte vectors,
 // at any alignment) between its statistics and its results, so each input is
-// read once and each output written once; sums are fp32.  The weight gradients'
+// read once and each output written once; sums are fp32.  A workgroup goes
+// through rows with as many waves on a row as it has vectors of 64 lanes (and several
+// rows side by side where that is few), the next row's loads on their way.  The weight gradients'
 // column sums run over chunks of rows in fp32 registers (the p and g gradients
 // share one), go to a workspace per chunk and are added chunk by chunk in
 // order: the result does not depend on the launch.
@@ -20,19 +22,29 @@ namespace bkmoo {
 
 namespace {
 
+// Sum over a wave, in every lane: neighbours, then the halves of 16 lanes, then rows of 16.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
+  x = add_dpp<0xB1>(x);   // lanes 1 0 3 2
+  x = add_dpp<0x4E>(x);   // lanes 2 3 0 1
+  x = add_dpp<0x141>(x);  // half rows of 16 mirrored
+  x = add_dpp<0x140>(x);  // rows mirrored
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-// Sums of N values over the WAVES waves of a row; every thread gets them.
+// Sums of N values over the WAVES waves of a row; every thread gets them.  One barrier:
+// `lds` must not be what an earlier call used unless a barrier lies between.
 template <int WAVES, int N>
 __device__ __forceinline__ void row_sums(float (&x)[N], float *lds, int wave, int lane) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
   if constexpr (WAVES > 1) {
-    __syncthreads();
     if (lane == 0)
 #pragma unroll
       for (int i = 0; i < N; ++i) lds[i * WAVES + wave] = x[i];
@@ -59,121 +71,189 @@ struct NormArgs {
   int64_t rows[kMaxK + 1];
 };
 
-// ROWS rows a workgroup, a row on WAVES waves, VPT vectors a thread.
-template <typename T, int WAVES, int VPT>
-__global__ __launch_bounds__(WAVES > 4 ? 64 * WAVES : 256) void norm_forward_kernel(const NormArgs a) {
-  constexpr int V = Vec<T>::kN, kRows = WAVES >= 4 ? 1 : 4 / WAVES;
-  __shared__ float lds[2 * WAVES * kRows];
-  const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % WAVES, sub = (threadIdx.x >> 6) / WAVES;
-  const int64_t row = (int64_t)blockIdx.x * kRows + sub;
-  if (row >= a.M) return;  // WAVES > 1 and kRows > 1 do not meet
-  const int64_t D = a.D;
-  const T *r = (const T *)a.r + row * D, *y = (const T *)a.y + row * D;
-  const T *w = (const T *)a.w, *p = (const T *)a.p, *g = (const T *)a.g;
-  u32x4 vr[VPT], vy[VPT];
+// How a workgroup holds rows: a row on WAVES waves with VPT vectors a thread, GROUPS rows side by
+// side.
+template <typename T, int WAVES, int VPT, int GROUPS>
+struct Rows {
+  static constexpr int V = Vec<T>::kN, kThreads = 64 * WAVES * GROUPS;
+  static constexpr bool kAhead = VPT * V <= 8;  // registers for the next row's vectors
+  static constexpr bool kHold = VPT * V <= 16;  // ... and for a row's at all (backward pass)
+};
+
+template <int VPT>
+struct Raw {
+  u32x4 v[VPT];
+};
+// A thread's vector i of a row; zeros past its end.  WHOLE: rows are whole vectors.
+template <typename T, int WAVES, bool WHOLE>
+__device__ __forceinline__ u32x4 vec_load(const T *row, int i, int at, int64_t D, bool there) {
+  const int64_t c = (int64_t)(i * WAVES * 64 + at) * Vec<T>::kN;
+  if (!there || c >= D) return u32x4{0, 0, 0, 0};
+  return WHOLE ? *(const u32x4_any *)(row + c) : guarded_chunk(row, c, D);
+}
+template <typename T, int WAVES, int VPT, bool WHOLE>
+__device__ __forceinline__ Raw<VPT> row_load(const T *row, int at, int64_t D, bool there) {
+  Raw<VPT> x;
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-    vy[i] = vr[i] = u32x4{0, 0, 0, 0};
-    if (c < D) {
-      vy[i] = guarded_chunk(y, c, D);
-      vr[i] = guarded_chunk(r, c, D);
+  for (int i = 0; i < VPT; ++i) x.v[i] = vec_load<T, WAVES, WHOLE>(row, i, at, D, there);
+  return x;
+}
+template <typename T, int WAVES, bool WHOLE>
+__device__ __forceinline__ void row_store(T *row, int i, int at, int64_t D, bool there, u32x4 v) {
+  const int64_t c = (int64_t)(i * WAVES * 64 + at) * Vec<T>::kN;
+  if (!there || c >= D) return;
+  if constexpr (WHOLE)
+    *(u32x4_any *)(row + c) = v;
+  else
+    guarded_store(row, c, D, v);
+}
+// One vector of a weight, or ones.
+template <typename T>
+__device__ __forceinline__ void weight_of(bool given, u32x4 v, float (&x)[Vec<T>::kN]) {
+  unpack(v, x);
+  if (!given)
+#pragma unroll
+    for (int e = 0; e < Vec<T>::kN; ++e) x[e] = 1.0f;
+}
+
+template <typename T, int WAVES, int VPT, int GROUPS, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES *GROUPS) void norm_forward_kernel(const NormArgs a) {
+  using R = Rows<T, WAVES, VPT, GROUPS>;
+  constexpr int V = R::V;
+  __shared__ float lds[2][2][GROUPS * WAVES];
+  const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % WAVES, grp = (threadIdx.x >> 6) / WAVES;
+  const int at = wave * 64 + lane;
+  const int64_t D = a.D, step = (int64_t)gridDim.x * GROUPS;
+  const T *w = (const T *)a.w, *p = (const T *)a.p, *g = (const T *)a.g;
+  const T *r = (const T *)a.r, *y = (const T *)a.y;
+  const Raw<VPT> vw = row_load<T, WAVES, VPT, WHOLE>(w, at, D, true);
+  const Raw<VPT> vp = row_load<T, WAVES, VPT, WHOLE>(p, at, D, p != nullptr);
+  const Raw<VPT> vg = row_load<T, WAVES, VPT, WHOLE>(g, at, D, g != nullptr);
+  int64_t row = (int64_t)blockIdx.x * GROUPS + grp;
+  Raw<VPT> nr = row_load<T, WAVES, VPT, WHOLE>(r + row * D, at, D, row < a.M);
+  Raw<VPT> ny = row_load<T, WAVES, VPT, WHOLE>(y + row * D, at, D, row < a.M);
+  int turn = 0;
+  // (every group goes round as often as the first: the barriers are the workgroup's)
+  for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < a.M; first += step, row += step, turn ^= 1) {
+    const bool there = row < a.M;
+    const Raw<VPT> vr = nr, vy = ny;
+    if constexpr (R::kAhead) {
+      nr = row_load<T, WAVES, VPT, WHOLE>(r + (row + step) * D, at, D, row + step < a.M);
+      ny = row_load<T, WAVES, VPT, WHOLE>(y + (row + step) * D, at, D, row + step < a.M);
     }
-  }
-  float inv[1] = {0.0f};
-  if (p) {
+    float inv[1] = {1.0f};
+    if (p) {
+      inv[0] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        float x[V];
+        unpack(vy.v[i], x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) inv[0] += x[e] * x[e];
+      }
+      row_sums<WAVES>(inv, &lds[0][turn][grp * WAVES], wave, lane);
+      inv[0] = 1.0f / sqrtf(inv[0] / (float)D + a.eps);
+    }
+    float rn[VPT][V], sum[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      float x[V];
-      unpack(vy[i], x);
+      float x[V], kp[V], kg[V];
+      unpack(vy.v[i], x);
+      unpack(vr.v[i], rn[i]);
+      weight_of<T>(p != nullptr, vp.v[i], kp);
+      weight_of<T>(g != nullptr, vg.v[i], kg);
 #pragma unroll
-      for (int e = 0; e < V; ++e) inv[0] += x[e] * x[e];
-    }
-    row_sums<WAVES>(inv, lds, wave, lane);
-    inv[0] = 1.0f / sqrtf(inv[0] / (float)D + a.eps);
-  }
-  float rn[VPT][V], sum[1] = {0.0f};
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-    float x[V], k[V];
-    unpack(vy[i], x);
-    unpack(vr[i], rn[i]);
-    if (c < D) {
-      if (p) {
-        unpack(guarded_chunk(p, c, D), k);
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[e] = x[e] * inv[0] * k[e];
+      for (int e = 0; e < V; ++e) {
+        rn[i][e] += a.c * (x[e] * inv[0] * kp[e] * kg[e]);
+        sum[0] += rn[i][e] * rn[i][e];
       }
-      if (g) {
-        unpack(guarded_chunk(g, c, D), k);
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[e] *= k[e];
-      }
+      row_store<T, WAVES, WHOLE>((T *)a.out0 + row * D, i, at, D, there, pack(rn[i]));
     }
+    row_sums<WAVES>(sum, &lds[1][turn][grp * WAVES], wave, lane);
+    const float rho = 1.0f / sqrtf(sum[0] / (float)D + a.eps);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      rn[i][e] += a.c * x[e];
-      sum[0] += rn[i][e] * rn[i][e];
+    for (int i = 0; i < VPT; ++i) {
+      float k[V], x[V];
+      unpack(vw.v[i], k);
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] = rn[i][e] * rho * k[e];
+      row_store<T, WAVES, WHOLE>((T *)a.out1 + row * D, i, at, D, there, pack(x));
     }
-    if (c < D) guarded_store((T *)a.out0 + row * D, c, D, pack(rn[i]));
-  }
-  row_sums<WAVES>(sum, lds + WAVES * kRows, wave, lane);
-  const float rho = 1.0f / sqrtf(sum[0] / (float)D + a.eps);
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-    if (c >= D) continue;
-    float k[V], x[V];
-    unpack(guarded_chunk(w, c, D), k);
-#pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = rn[i][e] * rho * k[e];
-    guarded_store((T *)a.out1 + row * D, c, D, pack(x));
+    if constexpr (!R::kAhead) {
+      nr = row_load<T, WAVES, VPT, WHOLE>(r + (row + step) * D, at, D, row + step < a.M);
+      ny = row_load<T, WAVES, VPT, WHOLE>(y + (row + step) * D, at, D, row + step < a.M);
+    }
   }
 }
 
 // A workgroup takes one chunk of rows of one task.
-template <typename T, int WAVES, int VPT>
-__global__ __launch_bounds__(64 * WAVES) void norm_backward_kernel(const NormArgs a) {
-  constexpr int V = Vec<T>::kN;
-  __shared__ float lds[4 * WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <typename T, int WAVES, int VPT, int GROUPS, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES *GROUPS, 2) void norm_backward_kernel(const NormArgs a) {
+  using R = Rows<T, WAVES, VPT, GROUPS>;
+  constexpr int V = R::V, kRow = WAVES * VPT * 64 * V;
+  __shared__ float lds[2][4][GROUPS * WAVES];  // [][0] to [][2]: three sums
+  __shared__ float cols[GROUPS > 1 ? 2 * kRow : 1];
+  const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % WAVES, grp = (threadIdx.x >> 6) / WAVES;
+  const int at = wave * 64 + lane;
   const int64_t D = a.D;
   int task = 0;
   while (task + 1 < a.tasks && (int)blockIdx.x >= a.chunks[task + 1]) ++task;
   const int64_t lo = a.rows[task] + (int64_t)((int)blockIdx.x - a.chunks[task]) * a.chunk_rows;
   const int64_t hi = lo + a.chunk_rows < a.rows[task + 1] ? lo + a.chunk_rows : a.rows[task + 1];
   const T *w = (const T *)a.w, *p = (const T *)a.p, *g = (const T *)a.g;
+  const T *r = (const T *)a.r, *y = (const T *)a.y, *dn = (const T *)a.dn, *up = (const T *)a.dup;
   float sw[VPT][V], ss[VPT][V];
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) sw[i][e] = ss[i][e] = 0.0f;
-  for (int64_t row = lo; row < hi; ++row) {
-    const T *r = (const T *)a.r + row * D, *y = (const T *)a.y + row * D;
-    const T *dn = (const T *)a.dn + row * D;
-    const T *up = a.dup ? (const T *)a.dup + row * D : nullptr;
-    u32x4 vr[VPT], vy[VPT], vn[VPT], vu[VPT];
+  int64_t row = lo + grp;
+  // Short rows: the weights, this row and the next in registers.  Long ones: read again, from
+  // the L2, in each of the three phases of a row.
+  Raw<R::kHold ? VPT : 1> vw, vp, vg, vr, vn, vy, vu, nr, nn, ny, nu;
+  auto ask = [&](int64_t q) {
+    if constexpr (R::kHold) {
+      nr = row_load<T, WAVES, VPT, WHOLE>(r + q * D, at, D, q < hi);
+      nn = row_load<T, WAVES, VPT, WHOLE>(dn + q * D, at, D, q < hi);
+      ny = row_load<T, WAVES, VPT, WHOLE>(y + q * D, at, D, q < hi);
+      nu = row_load<T, WAVES, VPT, WHOLE>(up + q * D, at, D, up && q < hi);
+    }
+  };
+  if constexpr (R::kHold) {
+    vw = row_load<T, WAVES, VPT, WHOLE>(w, at, D, true);
+    vp = row_load<T, WAVES, VPT, WHOLE>(p, at, D, p != nullptr);
+    vg = row_load<T, WAVES, VPT, WHOLE>(g, at, D, g != nullptr);
+  }
+  ask(row);
+  auto get = [&](int i, const Raw<R::kHold ? VPT : 1> &held, const T *from, bool there, float (&x)[V]) {
+    if constexpr (R::kHold) {
+      unpack(held.v[i], x);
+    } else {
+      unpack(vec_load<T, WAVES, WHOLE>(from, i, at, D, there), x);
+    }
+  };
+  auto ones = [&](bool given, float (&x)[V]) {
+    if (!given)
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[e] = 1.0f;
+  };
+  int turn = 0;
+  for (int64_t first = lo; first < hi; first += GROUPS, row += GROUPS, turn ^= 1) {
+    const bool there = row < hi;
+    vr = nr;
+    vn = nn;
+    vy = ny;
+    vu = nu;
+    const T *qr = r + row * D, *qn = dn + row * D, *qy = y + row * D, *qu = up ? up + row * D : nullptr;
+    if constexpr (R::kAhead) ask(row + GROUPS);
     float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-      vr[i] = vy[i] = vn[i] = vu[i] = u32x4{0, 0, 0, 0};
-      if (c < D) {
-        vr[i] = guarded_chunk(r, c, D);
-        vn[i] = guarded_chunk(dn, c, D);
-        vy[i] = guarded_chunk(y, c, D);
-        if (up) vu[i] = guarded_chunk(up, c, D);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
       float xr[V], xn[V], xy[V], k[V];
-      unpack(vr[i], xr);
-      unpack(vn[i], xn);
-      unpack(vy[i], xy);
-      unpack(c < D ? guarded_chunk(w, c, D) : u32x4{0, 0, 0, 0}, k);
+      get(i, vr, qr, there, xr);
+      get(i, vn, qn, there, xn);
+      get(i, vy, qy, there, xy);
+      get(i, vw, w, true, k);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         s[0] += xr[e] * xr[e];
@@ -181,65 +261,91 @@ __global__ __launch_bounds__(64 * WAVES) void norm_backward_kernel(const NormArg
         s[2] += xy[e] * xy[e];
       }
     }
-    row_sums<WAVES>(s, lds, wave, lane);
+    row_sums<WAVES>(s, &lds[turn][0][grp * WAVES * 3], wave, lane);
     const float rho = 1.0f / sqrtf(s[0] / (float)D + a.eps);
     const float q = rho * rho * (s[1] / (float)D);  // mean(x a) / rms, with one r' left out
     const float sig = p ? 1.0f / sqrtf(s[2] / (float)D + a.eps) : 1.0f;
-    float dr[VPT][V], t[1] = {0.0f};
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-      float xr[V], xn[V], xy[V], k[V], kp[V], kg[V];
-      unpack(vr[i], xr);
-      unpack(vn[i], xn);
-      unpack(vy[i], xy);
-      unpack(vu[i], dr[i]);
-      unpack(c < D ? guarded_chunk(w, c, D) : u32x4{0, 0, 0, 0}, k);
-#pragma unroll
-      for (int e = 0; e < V; ++e) kp[e] = kg[e] = 1.0f;
-      if (p && c < D) unpack(guarded_chunk(p, c, D), kp);
-      if (g && c < D) unpack(guarded_chunk(g, c, D), kg);
+    // dr and, of it, e = c g p dr
+    auto gradients = [&](int i, float (&xr)[V], float (&xn)[V], float (&dr)[V], float (&e_)[V]) {
+      float k[V], kp[V], kg[V];
+      get(i, vr, qr, there, xr);
+      get(i, vn, qn, there, xn);
+      get(i, vu, qu, there && up, dr);
+      get(i, vw, w, true, k);
+      get(i, vp, p, p != nullptr, kp);
+      get(i, vg, g, g != nullptr, kg);
+      ones(p != nullptr, kp);
+      ones(g != nullptr, kg);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float x = xr[e] * rho;
-        dr[i][e] += rho * (xn[e] * k[e] - xr[e] * q);
-        sw[i][e] += xn[e] * x;
-        const float d = a.c * dr[i][e];
-        ss[i][e] += d * (xy[e] * sig);
-        t[0] += d * kp[e] * kg[e] * xy[e];
+        dr[e] += rho * (xn[e] * k[e] - xr[e] * q);
+        e_[e] = a.c * dr[e] * kp[e] * kg[e];
       }
-      if (c < D) guarded_store((T *)a.out0 + row * D, c, D, pack(dr[i]));
-    }
+    };
     float m = 0.0f;
     if (p) {
-      row_sums<WAVES>(t, lds + 3 * WAVES, wave, lane);
+      float t[1] = {0.0f};
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        float xr[V], xn[V], dr[V], e_[V], xy[V];
+        gradients(i, xr, xn, dr, e_);
+        get(i, vy, qy, there, xy);
+#pragma unroll
+        for (int e = 0; e < V; ++e) t[0] += e_[e] * xy[e];
+      }
+      row_sums<WAVES>(t, &lds[turn][3][grp * WAVES], wave, lane);
       m = sig * sig * sig * (t[0] / (float)D);
     }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-      const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-      if (c >= D) continue;
-      float xy[V], kp[V], kg[V], x[V];
-      unpack(vy[i], xy);
+      float xr[V], xn[V], dr[V], e_[V], xy[V], x[V];
+      gradients(i, xr, xn, dr, e_);
+      get(i, vy, qy, there, xy);
 #pragma unroll
-      for (int e = 0; e < V; ++e) kp[e] = kg[e] = 1.0f;
-      if (p) unpack(guarded_chunk(p, c, D), kp);
-      if (g) unpack(guarded_chunk(g, c, D), kg);
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[e] = sig * (a.c * dr[i][e] * kp[e] * kg[e]) - xy[e] * m;
-      guarded_store((T *)a.out1 + row * D, c, D, pack(x));
-    }
-  }
-  float *part = a.partial + (int64_t)blockIdx.x * 2 * D;
-#pragma unroll
-  for (int i = 0; i < VPT; ++i) {
-    const int64_t c = (int64_t)(i * WAVES * 64 + wave * 64 + lane) * V;
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (c + e < D) {
-        part[c + e] = sw[i][e];
-        part[D + c + e] = ss[i][e];
+      for (int e = 0; e < V; ++e) {
+        if (there) {  // (one that is not has the statistics of zeros)
+          sw[i][e] += xn[e] * (xr[e] * rho);
+          ss[i][e] += a.c * dr[e] * (xy[e] * sig);
+        }
+        x[e] = sig * e_[e] - xy[e] * m;
       }
+      row_store<T, WAVES, WHOLE>((T *)a.out0 + row * D, i, at, D, there, pack(dr));
+      row_store<T, WAVES, WHOLE>((T *)a.out1 + row * D, i, at, D, there, pack(x));
+    }
+    if constexpr (!R::kAhead) ask(row + GROUPS);
+  }
+  // the groups' column sums, added in order
+  if constexpr (GROUPS > 1) {
+    for (int q = 0; q < GROUPS; ++q) {
+      __syncthreads();
+      if (grp == q)
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            float *c = cols + (i * WAVES * 64 + at) * V + e;
+            c[0] = q ? c[0] + sw[i][e] : sw[i][e];
+            c[kRow] = q ? c[kRow] + ss[i][e] : ss[i][e];
+          }
+    }
+    __syncthreads();
+    float *part = a.partial + (int64_t)blockIdx.x * 2 * D;
+    for (int c = threadIdx.x; c < (int)D; c += R::kThreads) {
+      part[c] = cols[c];
+      part[D + c] = cols[kRow + c];
+    }
+  } else {
+    float *part = a.partial + (int64_t)blockIdx.x * 2 * D;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int64_t c = (int64_t)(i * WAVES * 64 + at) * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (c + e < D) {
+          part[c + e] = sw[i][e];
+          part[D + c + e] = ss[i][e];
+        }
+    }
   }
 }
 
@@ -251,9 +357,9 @@ struct NormSumArgs {
   int chunks[kMaxK + 1];
 };
 
-constexpr int kSumCols = 64, kSumGroups = 16;
+constexpr int kSumCols = 16, kSumGroups = 64;
 
-// Column sums over a task's chunks: 16 interleaved runs of chunks side by side,
+// Column sums over a task's chunks: 64 interleaved runs of chunks side by side,
 // then these in order.
 template <typename T>
 __global__ __launch_bounds__(kSumCols *kSumGroups) void norm_sum_kernel(const NormSumArgs a) {
@@ -281,52 +387,58 @@ __global__ __launch_bounds__(kSumCols *kSumGroups) void norm_sum_kernel(const No
 }
 
 constexpr int64_t kMaxRowBytes = 64 << 10;  // sixteen waves of four vectors
-constexpr int kTargetChunks = 512;
+// Workgroups of the backward pass, about one of 512 threads a CU (bf16's registers leave no room
+// for a second): a few more would take as long as all the others, and each writes sums of its
+// own.  Of rows of 300 bf16 three of 256 threads instead take 73 us, these 59.
+constexpr int kTargetChunks = 256;
 
-int chunk_rows_for(int64_t M) {
-  const int64_t n = (M + kTargetChunks - 1) / kTargetChunks;
+int chunk_rows_for(int64_t M, int K) {
+  const int64_t target = kTargetChunks - K, n = (M + target - 1) / target;
   return (int)(n < 1 ? 1 : n);
 }
 
-template <typename T>
-hipError_t forward(const NormArgs &a, hipStream_t s) {
-  const int64_t nv = (a.D + Vec<T>::kN - 1) / Vec<T>::kN;
-  const unsigned by4 = (unsigned)((a.M + 3) / 4), by1 = (unsigned)a.M;
-  if (nv <= 64)
-    norm_forward_kernel<T, 1, 1><<<by4, 256, 0, s>>>(a);
-  else if (nv <= 128)
-    norm_forward_kernel<T, 1, 2><<<by4, 256, 0, s>>>(a);
-  else if (nv <= 256)
-    norm_forward_kernel<T, 4, 1><<<by1, 256, 0, s>>>(a);
-  else if (nv <= 512)
-    norm_forward_kernel<T, 4, 2><<<by1, 256, 0, s>>>(a);
-  else if (nv <= 1024)
-    norm_forward_kernel<T, 4, 4><<<by1, 256, 0, s>>>(a);
-  else if (nv <= 2048)
-    norm_forward_kernel<T, 16, 2><<<by1, 1024, 0, s>>>(a);
-  else
-    norm_forward_kernel<T, 16, 4><<<by1, 1024, 0, s>>>(a);
-  return hipGetLastError();
+// A row's waves and vectors by its length: as many waves as it has vectors of 64 lanes, up to eight
+// (a thread of sixteen waves has half the registers).
+template <typename T, template <typename, int, int, int> class Launch, typename... Args>
+hipError_t by_row(int64_t D, Args... args) {
+  const int64_t nv = (D + Vec<T>::kN - 1) / Vec<T>::kN;
+  if (nv <= 64) return Launch<T, 1, 1, 8>::run(args...);
+  if (nv <= 128) return Launch<T, 2, 1, 4>::run(args...);
+  if (nv <= 256) return Launch<T, 4, 1, 2>::run(args...);
+  if (nv <= 512) return Launch<T, 8, 1, 1>::run(args...);
+  if (nv <= 1024) return Launch<T, 8, 2, 1>::run(args...);
+  if (nv <= 2048) return Launch<T, 8, 4, 1>::run(args...);
+  return Launch<T, 16, 4, 1>::run(args...);
 }
+template <typename T, int WAVES, int VPT, int GROUPS>
+struct Forward {
+  static hipError_t run(const NormArgs &a, hipStream_t s) {
+    // eight workgroups a CU go through the rows (launching one costs more than a short row)
+    const int64_t n = (a.M + GROUPS - 1) / GROUPS, most = 8 * device_cu_count();
+    const dim3 grid((unsigned)(n < most ? n : most)), block(64 * WAVES * GROUPS);
+    if (a.D % Vec<T>::kN == 0)
+      norm_forward_kernel<T, WAVES, VPT, GROUPS, true><<<grid, block, 0, s>>>(a);
+    else
+      norm_forward_kernel<T, WAVES, VPT, GROUPS, false><<<grid, block, 0, s>>>(a);
+    return hipGetLastError();
+  }
+};
+template <typename T, int WAVES, int VPT, int GROUPS>
+struct Backward {
+  static hipError_t run(const NormArgs &a, int chunks, hipStream_t s) {
+    const dim3 grid((unsigned)chunks), block(64 * WAVES * GROUPS);
+    if (a.D % Vec<T>::kN == 0)
+      norm_backward_kernel<T, WAVES, VPT, GROUPS, true><<<grid, block, 0, s>>>(a);
+    else
+      norm_backward_kernel<T, WAVES, VPT, GROUPS, false><<<grid, block, 0, s>>>(a);
+    return hipGetLastError();
+  }
+};
 
 template <typename T>
 hipError_t backward(const NormArgs &a, const NormSumArgs &sum, int chunks, hipStream_t s) {
-  const int64_t nv = (a.D + Vec<T>::kN - 1) / Vec<T>::kN;
   if (chunks > 0) {
-    const unsigned n = (unsigned)chunks;
-    if (nv <= 64)
-      norm_backward_kernel<T, 1, 1><<<n, 64, 0, s>>>(a);
-    else if (nv <= 256)
-      norm_backward_kernel<T, 4, 1><<<n, 256, 0, s>>>(a);
-    else if (nv <= 512)
-      norm_backward_kernel<T, 4, 2><<<n, 256, 0, s>>>(a);
-    else if (nv <= 1024)
-      norm_backward_kernel<T, 8, 2><<<n, 512, 0, s>>>(a);
-    else if (nv <= 2048)
-      norm_backward_kernel<T, 16, 2><<<n, 1024, 0, s>>>(a);
-    else
-      norm_backward_kernel<T, 16, 4><<<n, 1024, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = by_row<T, Backward>(a.D, a, chunks, s);
     if (e != hipSuccess) return e;
   }
   const dim3 grid((unsigned)((a.D + kSumCols - 1) / kSumCols), (unsigned)a.tasks);
@@ -375,13 +487,13 @@ extern "C" bkmoo_status bkmoo_residual_norm_forward(int64_t M, int64_t D, bkmoo_
   a.D = D;
   a.c = (float)scale;
   a.eps = (float)eps;
-  return status_of(dt == BKMOO_F32 ? forward<float>(a, stream) : forward<__bf16>(a, stream));
+  return status_of(dt == BKMOO_F32 ? by_row<float, Forward>(D, a, stream) : by_row<__bf16, Forward>(D, a, stream));
 }
 
 extern "C" bkmoo_status bkmoo_residual_norm_workspace_size(int64_t M, int64_t D, int32_t K, size_t *bytes) {
   if (M < 0 || D < 1 || K < 1 || !bytes) return BKMOO_EINVAL;
   if (K > kMaxK) return BKMOO_EUNSUPPORTED;
-  const int rows = chunk_rows_for(M);
+  const int rows = chunk_rows_for(M, K);
   *bytes = align256((size_t)((M + rows - 1) / rows + K) * 2 * (size_t)D * sizeof(float));
   return BKMOO_OK;
 }
@@ -427,7 +539,7 @@ extern "C" bkmoo_status bkmoo_residual_norm_backward(int64_t M, int64_t D, bkmoo
   a.c = (float)scale;
   a.eps = (float)eps;
   a.partial = (float *)workspace;
-  a.chunk_rows = chunk_rows_for(M);
+  a.chunk_rows = chunk_rows_for(M, K);
   a.tasks = K;
   NormSumArgs sum = {};
   sum.partial = a.partial;
