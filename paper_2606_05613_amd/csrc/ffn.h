@@ -27,10 +27,11 @@ struct TileArgs {
   int64_t rows[kMaxK + 1];  // kWeightGrad: the tasks' rows
 };
 
-hipError_t launch_ffn_tile_f32(Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s);
-hipError_t launch_ffn_tile_bf16(Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s);
-// aligned: operands start at 16 bytes and so do all their rows.  wide: 256 x 256 tiles.
-hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s);
+hipError_t launch_ffn_tile_f32(Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s);
+hipError_t launch_ffn_tile_bf16(Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s);
+// aligned: operands start at 16 bytes and so do all their rows.  side: of the tiles, 64, 128 or
+// (aligned) 256.
+hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s);
 
 // The whole forward pass for at most kFewRows rows; h [M][F] is scratch.  More rows take the
 // tiles (us in all, D=4096 F=14336: 64 rows 95 here, 65 as tiles 110, 96 114 where here is about

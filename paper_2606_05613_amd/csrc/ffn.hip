@@ -12,44 +12,79 @@ constexpr int64_t kMaxWidth = 1 << 20;
 constexpr int kCus = 256;        // MI355X
 constexpr int kMaxSplits = 16;
 
-// The parts that a product's sum over k is cut into where its tiles alone leave most
-// of the chip idle: partial sums in fp32, added in order by split_sum_kernel.
-int split_count(int64_t M, int64_t N, int64_t K, int dt, bool wide) {
-  const int64_t side = wide ? 256 : 128, tiles = ((M + side - 1) / side) * ((N + side - 1) / side);
+// How a product is cut: tiles of side x side, the sum over k in `splits` parts (partial sums in
+// fp32, added in order by split_sum_kernel).
+struct Plan {
+  int side, splits;
+};
+
+// Estimated time of a product on `tiles` tiles of a CU, `steps` steps of 128 bytes along k each,
+// from times on MI355X.  bf16: a step of a tile of 256 takes a CU 1.8 us; of tiles of 128 one
+// 1.0 and two side by side 1.2, of 64 0.56 to 0.95 for one to four: small tiles lose to L2 and
+// LDS traffic, large ones to CUs without one.  fp32 is bound by the matrix cores at every
+// side.  The epilogue adds what its accesses take.  (us at 64 / 128 / 256, M x D x F: gate
+// and up 100 x 2048 x 6144 22 / 32 / 60, 1000 x 1024 x 3000 26 / 23 / 34, 512 x 4096 x 14336 240 /
+// 153 / 115; fp32 weight gradients 777 x 500 x 1364 42 / 46 / 82.)
+double product_us(int side, int dt, Mode mode, int64_t tiles, int64_t steps, bool aligned) {
+  const int64_t t = (tiles + kCus - 1) / kCus;  // of the busiest CU
+  static const double four[4] = {0.0, 0.56, 0.65, 0.8};
+  double step;
+  if (dt == F32)
+    step = side == 256 ? 7.2 * t : side == 128 ? 1.9 * t : t == 1 ? 0.6 : 0.5 * t;
+  else
+    step = side == 256 ? 1.8 * t : side == 128 ? 1.2 * (t / 2) + 1.0 * (t % 2) : 0.95 * (t / 4) + four[t % 4];
+  if (!aligned) step *= 1.5;
+  const double end = (side == 256 ? 8.0 : side == 128 ? 2.5 : 1.0) * (mode == kHiddenGrad ? 3.0 : 1.0);
+  return steps * step + t * end;
+}
+
+Plan plan(int dt, Mode mode, int64_t M, int64_t N, int64_t K, int64_t problems, bool aligned) {
+  Plan best = {128, 1};
+  double least = 0.0;
   const int64_t steps = (K * elem_bytes(dt) + 127) / 128;
-  int64_t n = kCus / (tiles < 1 ? 1 : tiles);
-  if (n > steps / 8) n = steps / 8;
-  if (n > kMaxSplits) n = kMaxSplits;
-  return n < 1 ? 1 : (int)n;
+  for (int side = aligned ? 256 : 128; side >= 64; side /= 2)
+    for (int splits = 1; splits <= kMaxSplits && (splits == 1 || steps / splits >= 4); splits *= 2) {
+      if (splits > 1 && mode != kDown && mode != kInputGrad) break;
+      const int64_t tiles = ((M + side - 1) / side) * ((N + side - 1) / side) * problems * splits;
+      double us = product_us(side, dt, mode, tiles, (steps + splits - 1) / splits, aligned);
+      if (splits > 1) us += 4.0 + 1.2e-6 * splits * M * N;  // written and read again, a launch
+      if (least == 0.0 || us < least) {
+        least = us;
+        best = Plan{side, splits};
+      }
+    }
+  return best;
 }
 
-// Wide (256 x 256) tiles move half the bytes through LDS for a product, but
-// leave CUs without one where there are few.
-bool wide_tiles(int64_t M, int64_t N, int64_t problems) {
-  return ((M + 255) / 256) * ((N + 255) / 256) * problems >= kCus;
-}
-
-__global__ __launch_bounds__(256) void split_sum_f32(const float *part, int splits, int64_t n, float *out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// Eight elements a thread: the parts in order, rounded once.
+template <typename T>
+__global__ __launch_bounds__(256) void split_sum_kernel(const float *part, int splits, int64_t n, T *out) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= n) return;
-  float s = part[i];
-  for (int k = 1; k < splits; ++k) s += part[k * n + i];
-  out[i] = s;
-}
-__global__ __launch_bounds__(256) void split_sum_bf16(const float *part, int splits, int64_t n, __bf16 *out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float s = part[i];
-  for (int k = 1; k < splits; ++k) s += part[k * n + i];
-  out[i] = (__bf16)s;
+  if (i + 8 <= n) {
+    float s[8], x[8];
+    load8(part + i).get(s);
+    for (int k = 1; k < splits; ++k) {
+      load8(part + k * n + i).get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += x[e];
+    }
+    store8(out + i, s);
+    return;
+  }
+  for (int64_t j = i; j < n; ++j) {
+    float s = part[j];
+    for (int k = 1; k < splits; ++k) s += part[k * n + j];
+    out[j] = (T)s;
+  }
 }
 
 hipError_t split_sum(int dt, const float *part, int splits, int64_t n, void *out, hipStream_t s) {
-  const unsigned grid = (unsigned)((n + 255) / 256);
+  const unsigned grid = (unsigned)((n + 2047) / 2048);
   if (dt == F32)
-    split_sum_f32<<<grid, 256, 0, s>>>(part, splits, n, (float *)out);
+    split_sum_kernel<<<grid, 256, 0, s>>>(part, splits, n, (float *)out);
   else
-    split_sum_bf16<<<grid, 256, 0, s>>>(part, splits, n, (__bf16 *)out);
+    split_sum_kernel<<<grid, 256, 0, s>>>(part, splits, n, (__bf16 *)out);
   return hipGetLastError();
 }
 
@@ -63,7 +98,9 @@ FfnLayout ffn_layout(int64_t M, int64_t D, int64_t F, int dt, bool backward) {
   L.du = mf;
   L.dv = L.du + (backward ? mf : 0);
   L.partial = L.dv + (backward ? mf : 0);
-  const int a = split_count(M, D, backward ? 2 * F : F, dt, true), b = split_count(M, D, backward ? 2 * F : F, dt, false);
+  const Mode mode = backward ? kInputGrad : kDown;
+  const int a = plan(dt, mode, M, D, backward ? 2 * F : F, 1, true).splits;
+  const int b = plan(dt, mode, M, D, backward ? 2 * F : F, 1, false).splits;
   const int splits = a > b ? a : b;
   L.total = L.partial + (splits > 1 ? align256((size_t)splits * M * D * sizeof(float)) : 0);
   return L;
@@ -78,23 +115,23 @@ bkmoo_status check_ffn(int64_t M, int64_t D, int64_t F, int dt, int act) {
 // y = h Wd^T or dx = du Wg + dv Wu, the sum split where that fills the chip.
 hipError_t narrow_product(int dt, Mode mode, TileArgs g, int64_t M, int64_t D, int64_t F, void *out, float *partial,
                           bool aligned, hipStream_t s) {
-  const bool wide = aligned && wide_tiles(M, D, 1);
+  const Plan p = plan(dt, mode, M, D, mode == kInputGrad ? 2 * F : F, 1, aligned);
   g.M = M;
   g.N = D;
   g.K = F;
   g.out[0] = out;
-  g.splits = split_count(M, D, mode == kInputGrad ? 2 * F : F, dt, wide);
+  g.splits = p.splits;
   g.partial = partial;
-  hipError_t e = launch_ffn_tile(dt, mode, g, 1, aligned, wide, s);
+  hipError_t e = launch_ffn_tile(dt, mode, g, 1, aligned, p.side, s);
   if (e == hipSuccess && g.splits > 1) e = split_sum(dt, partial, g.splits, M * D, out, s);
   return e;
 }
 
 }  // namespace
 
-hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s) {
-  return dt == F32 ? launch_ffn_tile_f32(mode, g, tasks, aligned, wide, s)
-                   : launch_ffn_tile_bf16(mode, g, tasks, aligned, wide, s);
+hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s) {
+  return dt == F32 ? launch_ffn_tile_f32(mode, g, tasks, aligned, side, s)
+                   : launch_ffn_tile_bf16(mode, g, tasks, aligned, side, s);
 }
 
 }  // namespace bkmoo
@@ -148,7 +185,7 @@ extern "C" bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo
   g.K = D;
   g.act = act == BKMOO_SILU ? kSilu : kGelu;
   g.splits = 1;
-  hipError_t e = launch_ffn_tile(dt, kGateUp, g, 1, aligned, aligned && wide_tiles(M, 2 * F, 1), stream);
+  hipError_t e = launch_ffn_tile(dt, kGateUp, g, 1, aligned, plan(dt, kGateUp, M, 2 * F, D, 1, aligned).side, stream);
   if (e != hipSuccess) return BKMOO_EHIP;
   TileArgs d = {};
   d.a[0] = ws + L.h;
@@ -198,7 +235,7 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
     g.K = D;
     g.act = act == BKMOO_SILU ? kSilu : kGelu;
     g.splits = 1;
-    e = launch_ffn_tile(dt, kHiddenGrad, g, 1, aligned, aligned && wide_tiles(M, F, 1), stream);
+    e = launch_ffn_tile(dt, kHiddenGrad, g, 1, aligned, plan(dt, kHiddenGrad, M, F, D, 1, aligned).side, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
     TileArgs d = {};
     d.a[0] = du;
@@ -223,5 +260,6 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
   w.task_stride = task_stride;
   w.splits = 1;
   for (int k = 0; k <= K; ++k) w.rows[k] = task_rows[k];
-  return status_of(launch_ffn_tile(dt, kWeightGrad, w, K, aligned, aligned && wide_tiles(F, D, 3 * K), stream));
+  return status_of(launch_ffn_tile(dt, kWeightGrad, w, K, aligned,
+                                   plan(dt, kWeightGrad, F, D, (M + K - 1) / K, 3 * K, aligned).side, stream));
 }

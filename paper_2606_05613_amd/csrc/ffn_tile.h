@@ -23,7 +23,8 @@
 //   K-contiguous  row r: 128 bytes, chunk c at place c ^ (r / 2 mod 8): the 16 rows
 //                 that a 128-bit fragment read touches at one c cover all banks once
 //   K-strided     row k: BM elements.  bf16: 32-byte segments s at place s ^ f(k), f the
-//                 eight rows that two 16-lane groups of a transposing read touch; fp32:
+//                 eight rows that two 16-lane groups of a transposing read touch (rows of 128
+//                 bytes: four of each parity); fp32:
 //                 64-byte segments at s ^ (k / 4 mod 4), the four rows of a 32-bit read
 // Fragments of K-strided bf16 operands come out of LDS through the transposing 64-bit
 // read (16 lanes read 4 k of 16 columns, lane i gets column i's 4 k).
@@ -64,7 +65,7 @@ struct Stage {
     if (KC)
       chunk = p ^ ((row >> 1) & 7);
     else if (kES == 2)
-      chunk = p ^ (2 * ((row & 3) | ((row >> 1) & 4)));
+      chunk = p ^ (2 * (W >= 128 ? (row & 3) | ((row >> 1) & 4) : ((row >> 1) & 1) | ((row >> 2) & 2)));
     else
       chunk = p ^ (4 * ((row >> 2) & 3));
   }
@@ -112,7 +113,8 @@ struct Reader {
     } else if constexpr (sizeof(T) == 2) {
       const int k = 8 * g + (j >> 2);
       base[0] = (uint32_t)(k * W * 2 + 8 * (j & 3));
-      x = (uint32_t)(32 * ((j >> 2) | ((g & 1) << 2))) ^ (uint32_t)(first * 2);
+      const int f = W >= 128 ? (j >> 2) | ((g & 1) << 2) : (j >> 3) | ((g & 1) << 1);
+      x = (uint32_t)(32 * f) ^ (uint32_t)(first * 2);
     } else {
       base[0] = (uint32_t)(4 * g * W * 4 + 4 * j);
       x = (uint32_t)(64 * g) ^ (uint32_t)(first * 4);
@@ -181,65 +183,81 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
                                            int64_t m0, int64_t n0, int64_t Mo, int64_t No, int wm, int wn, int lane) {
   constexpr bool GU = MODE == kGateUp;
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16, kHalf = GU ? BN / WN / 2 : 0;
-  // Inside the matrices two neighbouring pieces are exchanged between the lanes so
-  // that each holds eight consecutive columns: 16-byte accesses (bf16).  At an edge a
-  // lane writes its four columns of a piece one by one.
+  // Two neighbouring pieces are exchanged between the lanes so that each holds eight consecutive
+  // columns (kPairs of them a row of pieces): 16-byte accesses (bf16).  `whole`: all eight are
+  // there, n of them else.
   const int64_t mrow = m0 + wm * TM * 16 + (lane & 15);
-  const int64_t nwave = n0 + wn * (GU ? kHalf : TN * 16);
-  const int n4 = 4 * (lane >> 4), n8 = 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);
+  const int64_t nwave = n0 + wn * (GU ? kHalf : TN * 16) + 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);
   const bool inside = m0 + BM <= Mo && n0 + (GU ? BN / 2 : BN) <= No;
   constexpr int kPairs = (GU ? TN / 2 : TN) / 2;
-  if constexpr (MODE == kGateUp) {
-    T *h = (T *)g.out[0], *su = (T *)g.out[1], *sv = (T *)g.out[2];
-    const bool keep = su != nullptr;
-    if (inside) {
+  static_assert(kPairs > 0, "whole pairs of pieces");
+  auto each = [&](auto all, auto &&f) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int q = 0; q < kPairs; ++q) {
-          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
-          float u[8], v[8], x[8];
-          eight_columns(acc[i][2 * q], acc[i][2 * q + 1], u);
-          eight_columns(acc[i][TN / 2 + 2 * q], acc[i][TN / 2 + 2 * q + 1], v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = gate_act<T>(u[e], g.act) * v[e];
-          store8(h + at, x);
-          if (keep) {
-            store8(su + at, u);
-            store8(sv + at, v);
-          }
-        }
+      for (int q = 0; q < kPairs; ++q) {
+        const int64_t m = mrow + i * 16, n = nwave + q * 32;
+        const int64_t left = decltype(all)::value || m < Mo ? No - n : 0;
+        f(all, i, q, m * No + n, decltype(all)::value || left >= 8 ? 8 : left > 0 ? (int)left : 0);
+      }
+  };
+  auto everywhere = [&](auto &&f) {
+    if (inside)
+      each(std::true_type{}, f);
+    else
+      each(std::false_type{}, f);
+  };
+  // eight elements, or the first n of them
+  auto put = [](auto all, auto *p, const float (&x)[8], int n) {
+    using E = std::remove_reference_t<decltype(*p)>;
+    if (decltype(all)::value || n == 8) {
+      store8(p, x);
       return;
     }
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t m = mrow + i * 16;
-      if (m >= Mo) continue;
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = (E)x[e];
+  };
+  if constexpr (MODE == kGateUp) {
+    T *h = (T *)g.out[0], *su = (T *)g.out[1], *sv = (T *)g.out[2];
+    const bool keep = su != nullptr;
+    everywhere([&](auto all, int i, int q, int64_t at, int n) {
+      float u[8], v[8], x[8];
+      eight_columns(acc[i][2 * q], acc[i][2 * q + 1], u);
+      eight_columns(acc[i][TN / 2 + 2 * q], acc[i][TN / 2 + 2 * q + 1], v);
 #pragma unroll
-      for (int j = 0; j < TN / 2; ++j) {
-        const int64_t n = nwave + j * 16 + n4, at = m * No + n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < No) {
-            const float u = acc[i][j][e], v = acc[i][j + TN / 2][e];
-            h[at + e] = (T)(gate_act<T>(u, g.act) * v);
-            if (keep) {
-              su[at + e] = (T)u;
-              sv[at + e] = (T)v;
-            }
-          }
+      for (int e = 0; e < 8; ++e) x[e] = gate_act<T>(u[e], g.act) * v[e];
+      put(all, h + at, x, n);
+      if (keep) {
+        put(all, su + at, u, n);
+        put(all, sv + at, v, n);
       }
-    }
+    });
   } else if constexpr (MODE == kHiddenGrad) {
     const T *pu = (const T *)g.u, *pv = (const T *)g.v;
     T *du = (T *)g.out[0], *dv = (T *)g.out[1], *h = (T *)g.out[2];
+    auto finish = [&](auto all, int i, int q, int64_t at, int n, const float (&u)[8], const float (&v)[8]) {
+      float d[8], xu[8], xv[8], xh[8];
+      eight_columns(acc[i][2 * q], acc[i][2 * q + 1], d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float a, da;
+        gate_act_grad<T>(u[e], g.act, a, da);
+        xu[e] = d[e] * v[e] * da;
+        xv[e] = d[e] * a;
+        xh[e] = a * v[e];
+      }
+      put(all, du + at, xu, n);
+      put(all, dv + at, xv, n);
+      put(all, h + at, xh, n);
+    };
     if (inside) {
       // u and v of the next row of pieces travel while this one is worked on
       Eight<T> nu[2][kPairs], nv[2][kPairs];
       auto ask = [&](int i) {
 #pragma unroll
         for (int q = 0; q < kPairs; ++q) {
-          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
+          const int64_t at = (mrow + i * 16) * No + nwave + q * 32;
           nu[i & 1][q] = load8(pu + at);
           nv[i & 1][q] = load8(pv + at);
         }
@@ -250,82 +268,41 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
         if (i + 1 < TM) ask(i + 1);
 #pragma unroll
         for (int q = 0; q < kPairs; ++q) {
-          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
-          float d[8], u[8], v[8], xu[8], xv[8], xh[8];
-          eight_columns(acc[i][2 * q], acc[i][2 * q + 1], d);
+          float u[8], v[8];
           nu[i & 1][q].get(u);
           nv[i & 1][q].get(v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float a, da;
-            gate_act_grad<T>(u[e], g.act, a, da);
-            xu[e] = d[e] * v[e] * da;
-            xv[e] = d[e] * a;
-            xh[e] = a * v[e];
-          }
-          store8(du + at, xu);
-          store8(dv + at, xv);
-          store8(h + at, xh);
+          finish(std::true_type{}, i, q, (mrow + i * 16) * No + nwave + q * 32, 8, u, v);
         }
       }
-      return;
-    }
+    } else {
+      each(std::false_type{}, [&](auto all, int i, int q, int64_t at, int n) {
+        float u[8], v[8];
+        if (n == 8) {
+          load8(pu + at).get(u);
+          load8(pv + at).get(v);
+        } else {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t m = mrow + i * 16;
-      if (m >= Mo) continue;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int64_t n = nwave + j * 16 + n4, at = m * No + n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < No) {
-            const float d = acc[i][j][e], u = load1(pu + at + e), v = load1(pv + at + e);
-            float a, da;
-            gate_act_grad<T>(u, g.act, a, da);
-            du[at + e] = (T)(d * v * da);
-            dv[at + e] = (T)(d * a);
-            h[at + e] = (T)(a * v);
+          for (int e = 0; e < 8; ++e) {
+            u[e] = e < n ? load1(pu + at + e) : 0.0f;
+            v[e] = e < n ? load1(pv + at + e) : 0.0f;
           }
-      }
+        }
+        finish(all, i, q, at, n, u, v);
+      });
     }
   } else {
     T *out = MODE == kWeightGrad ? (T *)g.out[prob % 3] + (prob / 3) * g.task_stride : (T *)g.out[0];
     float *part = nullptr;
     if constexpr (MODE == kDown || MODE == kInputGrad)
       if (g.splits > 1) part = g.partial + (int64_t)prob * Mo * No;
-    if (inside) {
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int q = 0; q < kPairs; ++q) {
-          const int64_t at = (mrow + i * 16) * No + nwave + q * 32 + n8;
-          float x[8];
-          eight_columns(acc[i][2 * q], acc[i][2 * q + 1], x);
-          if (part)
-            store8(part + at, x);
-          else
-            store8(out + at, x);
-        }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t m = mrow + i * 16;
-      if (m >= Mo) continue;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int64_t n = nwave + j * 16 + n4, at = m * No + n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (n + e < No) {
-            if (part)
-              part[at + e] = acc[i][j][e];
-            else
-              out[at + e] = (T)acc[i][j][e];
-          }
-      }
-    }
+    everywhere([&](auto all, int i, int q, int64_t at, int n) {
+      float x[8];
+      eight_columns(acc[i][2 * q], acc[i][2 * q + 1], x);
+      if (part)
+        put(all, part + at, x, n);
+      else
+        put(all, out + at, x, n);
+    });
   }
 }
 
@@ -564,7 +541,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
   auto work = [&](auto half, auto loads, int buf, const Step &x) {
     constexpr int HALF = decltype(half)::value;
     constexpr bool LOAD = decltype(loads)::value;
-    constexpr int kReads = TM + TN, kEach = (kReads + TM - 3) / (TM - 2), kLoadEach = 2 * kLoads / TM;
+    constexpr int kReads = TM + TN, kEach = TM > 2 ? (kReads + TM - 3) / (TM - 2) : kReads;
+    constexpr int kLoadEach = TM > 1 ? 2 * kLoads / TM : kLoads;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll

@@ -5,30 +5,34 @@
 
 namespace bkmoo {
 
-// 256 x 256 tiles on eight waves, or 128 x 128 on four: see ffn_wide_tiles().
+// Tiles of 256 x 256 on eight waves, of 128 x 128 or 64 x 64 on four.
 template <typename T, Mode MODE, bool ALIGNED>
-hipError_t launch_mode(TileArgs g, int tasks, bool wide, hipStream_t s) {
+hipError_t launch_mode(TileArgs g, int tasks, int side, hipStream_t s) {
   const int64_t rows = g.M, cols = MODE == kGateUp ? 2 * g.N : g.N;
-  const int side = wide ? 256 : 128;
   g.tiles_m = (int)((rows + side - 1) / side);
   g.tiles_n = (int)((cols + side - 1) / side);
   g.problems = MODE == kWeightGrad ? 3 * tasks : g.splits > 1 ? g.splits : 1;
   const int64_t n = (int64_t)g.tiles_m * g.tiles_n * g.problems;
   if (n == 0) return hipSuccess;
   if (n > 0x3fffffff) return hipErrorInvalidConfiguration;
-  // As many workgroups as the chip holds at once (one of 512 threads or two of 256 a CU), each
-  // with tiles to the end: a tile's first steps travel while the one before is stored
+  // As many workgroups as the chip holds at once (a CU one of the largest, two of the next or four of
+  // the smallest), each with tiles to the end: a tile's first steps travel while the one before is stored
   // (M=4096, D=2048, F=6144, us, a workgroup a tile / these: gate and up 178 / 167, down 114 /
   // 95, weight gradients 324 / 301; 8192 x 4096 x 14336: 1772 / 1749, 857 / 852, 2564 / 2525).
   // The hidden gradient's epilogue waits for loads of its own, which the next tile's would
   // hold up: a workgroup a tile (963 / 1079).
   const int64_t cus = MODE == kHiddenGrad ? n : device_cu_count();
   if constexpr (ALIGNED) {
-    if (wide) {
+    if (side == 256) {
       const unsigned grid = (unsigned)(n < cus ? n : cus);
       ffn_tile_kernel<T, MODE, 256, 256, 2, 4, true><<<dim3(grid), dim3(512), 0, s>>>(g);
       return hipGetLastError();
     }
+  }
+  if (side == 64) {
+    const unsigned grid = (unsigned)(n < 4 * cus ? n : 4 * cus);
+    ffn_tile_kernel<T, MODE, 64, 64, 4, 1, ALIGNED><<<dim3(grid), dim3(256), 0, s>>>(g);
+    return hipGetLastError();
   }
   const unsigned grid = (unsigned)(n < 2 * cus ? n : 2 * cus);
   ffn_tile_kernel<T, MODE, 128, 128, 2, 2, ALIGNED><<<dim3(grid), dim3(256), 0, s>>>(g);
@@ -36,21 +40,21 @@ hipError_t launch_mode(TileArgs g, int tasks, bool wide, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_ffn_tile_of(Mode mode, const TileArgs &g, int tasks, bool aligned, bool wide, hipStream_t s) {
+hipError_t launch_ffn_tile_of(Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s) {
   switch (mode) {
     case kGateUp:
-      return aligned ? launch_mode<T, kGateUp, true>(g, tasks, wide, s) : launch_mode<T, kGateUp, false>(g, tasks, false, s);
+      return aligned ? launch_mode<T, kGateUp, true>(g, tasks, side, s) : launch_mode<T, kGateUp, false>(g, tasks, side, s);
     case kDown:
-      return aligned ? launch_mode<T, kDown, true>(g, tasks, wide, s) : launch_mode<T, kDown, false>(g, tasks, false, s);
+      return aligned ? launch_mode<T, kDown, true>(g, tasks, side, s) : launch_mode<T, kDown, false>(g, tasks, side, s);
     case kHiddenGrad:
-      return aligned ? launch_mode<T, kHiddenGrad, true>(g, tasks, wide, s)
-                     : launch_mode<T, kHiddenGrad, false>(g, tasks, false, s);
+      return aligned ? launch_mode<T, kHiddenGrad, true>(g, tasks, side, s)
+                     : launch_mode<T, kHiddenGrad, false>(g, tasks, side, s);
     case kInputGrad:
-      return aligned ? launch_mode<T, kInputGrad, true>(g, tasks, wide, s)
-                     : launch_mode<T, kInputGrad, false>(g, tasks, false, s);
+      return aligned ? launch_mode<T, kInputGrad, true>(g, tasks, side, s)
+                     : launch_mode<T, kInputGrad, false>(g, tasks, side, s);
     default:
-      return aligned ? launch_mode<T, kWeightGrad, true>(g, tasks, wide, s)
-                     : launch_mode<T, kWeightGrad, false>(g, tasks, false, s);
+      return aligned ? launch_mode<T, kWeightGrad, true>(g, tasks, side, s)
+                     : launch_mode<T, kWeightGrad, false>(g, tasks, side, s);
   }
 }
 
