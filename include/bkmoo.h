@@ -456,8 +456,8 @@ bkmoo_status bkmoo_set_wait_limit(uint32_t polls);
  *
  * Shared conventions: matrices are row-major and contiguous, of one type `dt`;
  * sums, statistics and activations are fp32, results rounded once to nearest
- * even; non-finite values propagate.  Pointers need natural alignment (rows that
- * start at 16 bytes take faster kernels); a workspace starts at 16 bytes and
+ * even; non-finite values propagate.  Pointers need natural alignment (matrices
+ * whose rows start at multiples of four bytes take faster kernels); a workspace starts at 16 bytes and
  * needs no initialisation.  task_rows (host) is int64[K+1] from 0 to M,
  * non-decreasing, 1 <= K <= 16; a task without rows gets zero gradients.  Weight gradient k
  * of a matrix starts task_stride elements after gradient k-1 (task_stride >=

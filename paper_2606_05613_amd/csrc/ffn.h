@@ -29,7 +29,7 @@ struct TileArgs {
 
 hipError_t launch_ffn_tile_f32(Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s);
 hipError_t launch_ffn_tile_bf16(Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s);
-// aligned: operands start at 16 bytes and so do all their rows.  side: of the tiles, 64, 128 or
+// aligned: operands start at multiples of four bytes and so do all their rows.  side: of the tiles, 64, 128 or
 // (aligned) 256.
 hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool aligned, int side, hipStream_t s);
 

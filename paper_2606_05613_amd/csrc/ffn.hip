@@ -168,8 +168,7 @@ extern "C" bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo
   if (any_overlap(in, out)) return BKMOO_EINVAL;
   if (M == 0) return BKMOO_OK;
   char *ws = (char *)workspace;
-  const int64_t v = 16 / (int64_t)es;
-  const bool aligned = D % v == 0 && F % v == 0 && at16(x) && at16(w_gate) && at16(w_up) && at16(w_down);
+  const bool aligned = D * es % 4 == 0 && F * es % 4 == 0 && at4(x) && at4(w_gate) && at4(w_up) && at4(w_down);
   if (M <= kFewRows)
     return status_of(launch_ffn_few(dt, x, w_gate, w_up, w_down, ws + L.h, y, gate_out, up_out, M, D, F,
                                     act == BKMOO_SILU ? kSilu : kGelu, aligned, stream));
@@ -218,8 +217,8 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
   if (any_overlap(in, out)) return BKMOO_EINVAL;
   char *ws = (char *)workspace;
   void *du = ws + L.du, *dv = ws + L.dv, *h = ws + L.h;
-  const int64_t v = 16 / (int64_t)es;
-  const bool aligned = D % v == 0 && F % v == 0 && at16(dy) && at16(x) && at16(w_gate) && at16(w_up) && at16(w_down);
+  const bool aligned =
+      D * es % 4 == 0 && F * es % 4 == 0 && at4(dy) && at4(x) && at4(w_gate) && at4(w_up) && at4(w_down);
   hipError_t e = hipSuccess;
   if (M > 0) {
     TileArgs g = {};

@@ -62,7 +62,7 @@ __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PA
 }
 
 // PAIR: both projections and the gate; else one product.  R: tiles of 16 columns, NT: tiles of 16
-// tokens.  Rows that do not start at 16 bytes: loads straight into the matrix instruction's
+// tokens.  Rows that do not start at four bytes: loads straight into the matrix instruction's
 // layout, at any alignment.  Lane l holds 16 bytes of weight row l mod 16, and the same bytes of
 // token l mod 16.  A step of a wave is 128 bytes of every row, in two loads that take turns
 // in the line (the order of k is the same for weights and tokens, and free).  U steps make a
@@ -214,6 +214,17 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FewArgs a) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     ask(slot == 0 ? DEPTH - 1 : slot - 1);
     wait_loads<(DEPTH - 1) * kLoads>();
+    if (const int rest = (int)K - s * BK; rest < BK && rest % V != 0) {
+      // the row ends inside a chunk: what was loaded of the next one is cleared
+#pragma unroll
+      for (int i = 0; i < W + NT; ++i) {
+        const uint32_t at = ring + slot * kSlot + i * 2048 + lane * 16;
+        const int keep0 = (rest - chunk0 * V) * ES, keep1 = (rest - chunk1 * V) * ES;
+        if (keep0 > 0 && keep0 < 16) keep_bytes(at, keep0);
+        if (keep1 > 0 && keep1 < 16) keep_bytes(at + 1024, keep1);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
     const BKMOO_LDS char *from = (const BKMOO_LDS char *)(uintptr_t)(ring + slot * kSlot);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {

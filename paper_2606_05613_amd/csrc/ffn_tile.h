@@ -16,7 +16,8 @@
 // while the second half of step t is multiplied: the barrier finds every wave with its
 // next operands in registers.  Rows past the end of a matrix fall outside the
 // descriptor's range and arrive as zeros; so do the chunks past K of a K-contiguous
-// operand.
+// operand, and a chunk that K ends in is cleaned in LDS.  (The loads need rows at
+// multiples of four bytes: rows of an odd number of bf16 go through registers instead.)
 //
 // LDS layouts (16-byte chunks; the loads fill LDS in lane order, so a layout is
 // made by choosing what each lane reads):
@@ -485,6 +486,27 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
     }
   };
 
+  // A step that ends inside a 16-byte chunk of its rows: what the loads brought of the next rows
+  // is cleared, by the lane that loaded it.
+  auto clear = [&](const Step &x) {
+    if ((!AKC && !BKC) || x.left >= BK || x.left % (16 / ES) == 0) return;
+    int at = lane;
+    asm volatile("" : "+v"(at));  // worked out here, once a tile: no registers for it in the loop
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const bool isa = i < SA::kPer;
+      if (isa ? !AKC : !BKC) continue;
+      const int q = isa ? i : i - SA::kPer;
+      int row, chunk;
+      if (isa)
+        SA::place(wave * SA::kPer + q, at, row, chunk);
+      else
+        SB::place(wave * SB::kPer + q, at, row, chunk);
+      const int keep = (x.left - chunk * (16 / ES)) * ES;
+      if (keep > 0 && keep < 16) keep_bytes((isa ? x.la : x.lb) + q * 1024 + at * 16, keep);
+    }
+  };
+
   // Steps through registers, element by element where a chunk crosses an end (!ALIGNED).
   u32x4 ra[ALIGNED ? 1 : SA::kPer], rb[ALIGNED ? 1 : SB::kPer];
   auto fetch = [&](const Tile &x, int t) {
@@ -561,16 +583,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
   using Second = std::integral_constant<int, 1>;
   using Loads = std::bool_constant<ALIGNED>;
 
-  Step x = {};
+  Step x = {}, ahead = {};  // ahead: the last one loaded
   if constexpr (ALIGNED) {
     start_tile(0);
-    for (int i = 0; i < 2; ++i) {
-      x = next_step(i);
+    x = next_step(0);
 #pragma unroll
-      for (int q = 0; q < kLoads; ++q) piece(x, q);
-      move_on();
-    }
+    for (int q = 0; q < kLoads; ++q) piece(x, q);
+    move_on();
+    ahead = next_step(1);
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) piece(ahead, q);
+    move_on();
     wait_loads<kLoads>();
+    clear(x);
     barrier_lds();
   }
   int buf = 0;
@@ -610,6 +635,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
         else
           wait_loads<0>();
         stored = false;
+        clear(ahead);
+        ahead = x;
       }
       barrier_lds();
       work(Second{}, Loads{}, buf ^ 1, x);  // (after the last step: reads what is there)

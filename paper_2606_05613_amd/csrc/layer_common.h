@@ -8,7 +8,7 @@ namespace bkmoo {
 
 inline bool valid_elem(int dt) { return dt == BKMOO_F32 || dt == BKMOO_BF16; }
 inline bool natural(const void *p, int dt) { return (uintptr_t)p % (uintptr_t)elem_bytes(dt) == 0; }
-inline bool at16(const void *p) { return (uintptr_t)p % 16 == 0; }
+inline bool at4(const void *p) { return (uintptr_t)p % 4 == 0; }
 
 // Bytes [p, p + n) of a call's inputs and outputs.
 struct Range {

@@ -44,6 +44,16 @@ __device__ __forceinline__ void wait_loads() {
 __device__ __forceinline__ void barrier_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+// A 16-byte chunk in LDS, loaded by this lane, of which only the first `keep` bytes belong to the
+// row: the rest becomes zero.
+__device__ __forceinline__ void keep_bytes(uint32_t lds, int keep) {
+  BKMOO_LDS uint32_t *p = (BKMOO_LDS uint32_t *)(uintptr_t)lds;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = keep - 4 * i;
+    if (b < 4) p[i] = b <= 0 ? 0 : p[i] & ((1u << (8 * b)) - 1);
+  }
+}
 constexpr uint32_t kNowhere = 0x80000000u;  // beyond every descriptor's range
 
 // Fragments: 16 rows (or columns) of an operand and 64 bytes of k; lane l holds 16 bytes of
