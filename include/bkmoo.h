@@ -551,7 +551,7 @@ bkmoo_status bkmoo_ffn_workspace_size(int64_t M, int64_t D, int64_t F, bkmoo_dty
  *   gate_out, up_out [M][F]                         (out, both or neither NULL) u and v,
  *                                                   for the backward pass
  *
- * For more than a few rows h is rounded to dt between the products.
+ * For more than eight rows h is rounded to dt between the products.
  * BKMOO_EUNSUPPORTED for D or F above 2^20.
  */
 bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, bkmoo_act act, const void *x,

@@ -93,7 +93,8 @@ struct FfnLayout {
 };
 FfnLayout ffn_layout(int64_t M, int64_t D, int64_t F, int dt, bool backward) {
   FfnLayout L;
-  const size_t mf = align256((size_t)M * F * elem_bytes(dt));
+  const bool two = !backward && dt == BF16 && M <= kFewExact;
+  const size_t mf = align256((size_t)M * F * elem_bytes(dt) * (two ? 2 : 1));
   L.h = 0;
   L.du = mf;
   L.dv = L.du + (backward ? mf : 0);

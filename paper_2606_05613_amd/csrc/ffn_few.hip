@@ -23,12 +23,18 @@ namespace {
 struct FewArgs {
   const void *x, *w0, *w1;     // [M][K]; [N][K] (w1: the up product's)
   void *out, *u, *v;           // [M][N]; u, v: may be null
+  void *lo;                    // [M][F] or null: what rounding h to T leaves out, rounded to T
   int64_t M, N, K;
   int act;
 };
 
+// h is what the two kernels pass on.  Up to eight tokens of bf16 pass it on as two bf16, the second
+// what rounding leaves out of the first (2^-17 of it is lost then): a token's errors come from a
+// few large elements of h and do not average out.  The second product takes both as the 16 tokens
+// of a tile (SPLIT), at no cost.
+
 // The waves' sums, added in wave order, and what becomes of them.
-template <typename T, bool PAIR, int R, int NT, int WAVES>
+template <typename T, bool PAIR, int R, int NT, int WAVES, bool SPLIT>
 __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PAIR ? 2 : 1) * R][NT][64], int64_t n0,
                                        int wave, int lane) {
   const int g = lane >> 4, r = lane & 15;
@@ -41,6 +47,9 @@ __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PA
       s[i] = sums[0][i * R + c][t][lane];
 #pragma unroll
       for (int q = 1; q < WAVES; ++q) s[i] += sums[q][i * R + c][t][lane];
+      if constexpr (SPLIT)
+#pragma unroll
+        for (int q = 0; q < WAVES; ++q) s[i] += sums[q][i * R + c][t][lane ^ 8];  // (token r + 8)
     }
     const int64_t m = t * 16 + r, n = n0 + c * 16 + 4 * g;
     if (m >= a.M) continue;
@@ -49,7 +58,9 @@ __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PA
     for (int e = 0; e < 4; ++e)
       if (n + e < a.N) {
         if constexpr (PAIR) {
-          ((T *)a.out)[at + e] = (T)(gate_act<T>(s[0][e], a.act) * s[1][e]);
+          const float h = gate_act<T>(s[0][e], a.act) * s[1][e];
+          ((T *)a.out)[at + e] = (T)h;
+          if (a.lo) ((T *)a.lo)[at + e] = (T)(__builtin_isfinite(h) ? h - (float)(T)h : 0.0f);
           if (a.u) {
             ((T *)a.u)[at + e] = (T)s[0][e];
             ((T *)a.v)[at + e] = (T)s[1][e];
@@ -67,7 +78,7 @@ __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PA
 // token l mod 16.  A step of a wave is 128 bytes of every row, in two loads that take turns
 // in the line (the order of k is the same for weights and tokens, and free).  U steps make a
 // batch; one batch travels while the one before is multiplied.
-template <typename T, bool PAIR, int R, int NT, int WAVES, int U>
+template <typename T, bool PAIR, int R, int NT, int WAVES, int U, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, 2) void ffn_few_any_kernel(const FewArgs a) {
   constexpr int V = 16 / sizeof(T), BK = 8 * V, W = (PAIR ? 2 : 1) * R;
   __shared__ f32x4 sums[WAVES][W][NT][64];
@@ -84,8 +95,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_few_any_kernel(const FewArg
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int64_t m = t * 16 + r < a.M ? t * 16 + r : a.M - 1;
-    x[t] = (const T *)a.x + m * K + g * 2 * V;
+    const int64_t mt = SPLIT ? r & 7 : t * 16 + r, m = mt < a.M ? mt : a.M - 1;
+    x[t] = (const T *)(SPLIT && r >= 8 ? a.lo : a.x) + m * K + g * 2 * V;
   }
   f32x4 acc[W][NT];
 #pragma unroll
@@ -148,12 +159,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void ffn_few_any_kernel(const FewArg
 #pragma unroll
     for (int t = 0; t < NT; ++t) sums[wave][i][t][lane] = acc[i][t];
   __syncthreads();
-  finish<T, PAIR, R, NT, WAVES>(a, sums, n0, wave, lane);
+  finish<T, PAIR, R, NT, WAVES, SPLIT>(a, sums, n0, wave, lane);
 }
 
 // The same through LDS: a wave's loads cover whole lines of eight rows, into a ring of DEPTH
 // steps of its own.
-template <typename T, bool PAIR, int R, int NT, int WAVES, int DEPTH>
+template <typename T, bool PAIR, int R, int NT, int WAVES, int DEPTH, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FewArgs a) {
   constexpr int ES = sizeof(T), V = 16 / ES, BK = 8 * V, W = (PAIR ? 2 : 1) * R;
   constexpr int kSlot = (W + NT) * 2048, kLoads = 2 * (W + NT), kSums = WAVES * W * NT * 1024;
@@ -172,13 +183,13 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FewArgs a) {
   const uint32_t off0 = row * ld + chunk0 * 16, off1 = (row + 8) * ld + chunk1 * 16;
   const char *pw[2] = {(const char *)a.w0 + (n0 * K + (int64_t)s0 * BK) * ES,
                        PAIR ? (const char *)a.w1 + (n0 * K + (int64_t)s0 * BK) * ES : nullptr};
-  const char *px = (const char *)a.x + (int64_t)s0 * 128;
+  const char *px = (const char *)a.x + (int64_t)s0 * 128, *pl = SPLIT ? (const char *)a.lo + (int64_t)s0 * 128 : px;
   int64_t wbytes = ((a.N - n0) * K - (int64_t)s0 * BK) * ES, xbytes = a.M * K * ES - (int64_t)s0 * 128;
   int left = (int)K - s0 * BK, asked = s0;
   auto ask = [&](int slot) {
     const bool any = asked < s1;  // else zeros, so that every step has its loads to count
     const i32x4 d0 = make_desc(pw[0], any ? wbytes : 0), d1 = make_desc(pw[PAIR ? 1 : 0], any ? wbytes : 0);
-    const i32x4 dx = make_desc(px, any ? xbytes : 0);
+    const i32x4 dx = make_desc(px, any ? xbytes : 0), dl = SPLIT ? make_desc(pl, any ? xbytes : 0) : dx;
     const uint32_t o0 = chunk0 * V < left ? off0 : kNowhere, o1 = chunk1 * V < left ? off1 : kNowhere;
     const uint32_t to = ring + slot * kSlot;
 #pragma unroll
@@ -190,11 +201,13 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FewArgs a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       load_to_lds(to + (W + t) * 2048, dx, o0 + t * 16 * ld);
-      load_to_lds(to + (W + t) * 2048 + 1024, dx, o1 + t * 16 * ld);
+      // (SPLIT: the second eight rows are the first of the other matrix)
+      load_to_lds(to + (W + t) * 2048 + 1024, dl, SPLIT && o1 != kNowhere ? o1 - 8 * ld : o1 + t * 16 * ld);
     }
     pw[0] += 128;
     pw[1] += 128;
     px += 128;
+    pl += 128;
     wbytes -= 128;
     xbytes -= 128;
     left -= BK;
@@ -249,7 +262,7 @@ __global__ __launch_bounds__(64 * WAVES) void ffn_few_kernel(const FewArgs a) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) sums[wave][i][t][lane] = acc[i][t];
   __syncthreads();
-  finish<T, PAIR, R, NT, WAVES>(a, sums, n0, wave, lane);
+  finish<T, PAIR, R, NT, WAVES, SPLIT>(a, sums, n0, wave, lane);
 }
 
 // Steps of the ring that fit into KB kilobytes of LDS, at most eight.
@@ -259,28 +272,33 @@ constexpr int kDepth = [] {
   return n > 8 ? 8 : n;
 }();
 
-template <typename T, bool PAIR, int R, int WAVES, int KB>
-hipError_t launch(const FewArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.N + 16 * R - 1) / (16 * R))), block(64 * WAVES);
-  if (a.M <= 16)
-    ffn_few_kernel<T, PAIR, R, 1, WAVES, kDepth<PAIR, R, 1, WAVES, KB>><<<grid, block, 0, s>>>(a);
-  else if (a.M <= 32)
-    ffn_few_kernel<T, PAIR, R, 2, WAVES, kDepth<PAIR, R, 2, WAVES, KB>><<<grid, block, 0, s>>>(a);
-  else
-    ffn_few_kernel<T, PAIR, R, 4, WAVES, kDepth<PAIR, R, 4, WAVES, KB>><<<grid, block, 0, s>>>(a);
+template <typename T, bool PAIR, int R, int NT, int WAVES, int KB, bool SPLIT = false>
+hipError_t launch_tiles(const FewArgs &a, hipStream_t s) {
+  ffn_few_kernel<T, PAIR, R, NT, WAVES, kDepth<PAIR, R, NT, WAVES, KB>, SPLIT>
+      <<<dim3((unsigned)((a.N + 16 * R - 1) / (16 * R))), dim3(64 * WAVES), 0, s>>>(a);
   return hipGetLastError();
 }
+template <typename T, bool PAIR, int R, int WAVES, int KB>
+hipError_t launch(const FewArgs &a, hipStream_t s) {
+  if constexpr (!PAIR && sizeof(T) == 2)
+    if (a.lo) return launch_tiles<T, PAIR, R, 1, WAVES, KB, true>(a, s);
+  return a.M <= 16   ? launch_tiles<T, PAIR, R, 1, WAVES, KB>(a, s)
+         : a.M <= 32 ? launch_tiles<T, PAIR, R, 2, WAVES, KB>(a, s)
+                     : launch_tiles<T, PAIR, R, 4, WAVES, KB>(a, s);
+}
 
+template <typename T, bool PAIR, int NT, int U, bool SPLIT = false>
+hipError_t launch_any_tiles(const FewArgs &a, hipStream_t s) {
+  ffn_few_any_kernel<T, PAIR, 1, NT, 4, U, SPLIT><<<dim3((unsigned)((a.N + 15) / 16)), dim3(256), 0, s>>>(a);
+  return hipGetLastError();
+}
 template <typename T, bool PAIR>
 hipError_t launch_any(const FewArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.N + 15) / 16)), block(256);
-  if (a.M <= 16)
-    ffn_few_any_kernel<T, PAIR, 1, 1, 4, 2><<<grid, block, 0, s>>>(a);
-  else if (a.M <= 32)
-    ffn_few_any_kernel<T, PAIR, 1, 2, 4, 1><<<grid, block, 0, s>>>(a);
-  else
-    ffn_few_any_kernel<T, PAIR, 1, 4, 4, 1><<<grid, block, 0, s>>>(a);
-  return hipGetLastError();
+  if constexpr (!PAIR && sizeof(T) == 2)
+    if (a.lo) return launch_any_tiles<T, PAIR, 1, 2, true>(a, s);
+  return a.M <= 16   ? launch_any_tiles<T, PAIR, 1, 2>(a, s)
+         : a.M <= 32 ? launch_any_tiles<T, PAIR, 2, 1>(a, s)
+                     : launch_any_tiles<T, PAIR, 4, 1>(a, s);
 }
 
 // Two tiles of columns a workgroup read the tokens half as often, but make half as many
@@ -303,7 +321,9 @@ hipError_t few(const FewArgs &pair, const FewArgs &down, bool aligned, hipStream
 
 hipError_t launch_ffn_few(int dt, const void *x, const void *wg, const void *wu, const void *wd, void *h, void *y,
                           void *u, void *v, int64_t M, int64_t D, int64_t F, int act, bool aligned, hipStream_t s) {
-  const FewArgs pair = {x, wg, wu, h, u, v, M, F, D, act}, down = {h, wd, nullptr, y, nullptr, nullptr, M, D, F, act};
+  void *lo = dt == BF16 && M <= kFewExact ? (char *)h + (size_t)M * F * elem_bytes(dt) : nullptr;
+  const FewArgs pair = {x, wg, wu, h, u, v, lo, M, F, D, act};
+  const FewArgs down = {h, wd, nullptr, y, nullptr, nullptr, lo, M, D, F, act};
   return dt == F32 ? few<float>(pair, down, aligned, s) : few<__bf16>(pair, down, aligned, s);
 }
 
