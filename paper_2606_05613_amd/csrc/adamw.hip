@@ -37,7 +37,7 @@ constexpr int kBlock = 256;             // elements that share a scale
 constexpr int kChunk = 4096;            // elements of a workgroup
 constexpr int kAdamThreads = 256;
 constexpr int kLaneElems = 8;
-constexpr int kMaxTensors = 120;
+constexpr int kMaxTensors = 192;
 constexpr double kFineBeta = 0.98;
 constexpr float kF8Max = 448.0f;
 constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: a block below it holds zeros
@@ -51,12 +51,12 @@ struct AdamArgs {
   uint32_t seed;
   int fine;                      // sixteen random bits a moment
   int n;                         // tensors of this launch
-  uint8_t decay[kMaxTensors];
+  int64_t start0, block0, total; // its first element in the flat vectors and block of 256, its elements
   void *p[kMaxTensors];
-  int64_t start[kMaxTensors + 1];  // first element in the flat vectors
-  int64_t block[kMaxTensors];    // first block of 256
-  int chunk[kMaxTensors + 1];    // first chunk
+  uint32_t start[kMaxTensors], block[kMaxTensors];  // of each tensor, from those on
+  uint32_t chunk[kMaxTensors];   // first chunk, and whether weight decay applies (kDecay)
 };
+constexpr uint32_t kDecay = 0x80000000u;
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -149,20 +149,20 @@ template <typename T, typename G, bool S8, bool MASTER>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   int t = 0;
   {
-    int hi = a.n;  // chunk[t] <= blockIdx.x < chunk[hi]
+    int hi = a.n;  // the chunks of t are at or before blockIdx.x, those of hi behind it
     while (hi - t > 1) {
       const int mid = (t + hi) >> 1;
-      if (a.chunk[mid] <= (int)blockIdx.x) t = mid; else hi = mid;
+      if ((a.chunk[mid] & ~kDecay) <= blockIdx.x) t = mid; else hi = mid;
     }
   }
-  const int64_t first = (int64_t)((int)blockIdx.x - a.chunk[t]) * kChunk;
-  const int64_t start = a.start[t], n = a.start[t + 1] - start;
+  const int64_t first = (int64_t)(blockIdx.x - (a.chunk[t] & ~kDecay)) * kChunk;
+  const int64_t start = a.start0 + a.start[t], n = (t + 1 < a.n ? (int64_t)a.start[t + 1] : a.total) - a.start[t];
   const int64_t end = first + kChunk < n ? first + kChunk : n;
   T *p = (T *)a.p[t];
   const G *grad = (const G *)a.grad + start;
   float *master = MASTER ? a.master + start : nullptr;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
-  const float keep = a.decay[t] ? a.keep : 1.0f;
+  const float keep = a.chunk[t] & kDecay ? a.keep : 1.0f;
   for (int64_t base = first; base < end; base += kAdamThreads * kLaneElems) {
     const int64_t i = base + threadIdx.x * kLaneElems;
     if (!S8 && i >= n) break;
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
       load8_of((const T *)p, i, n, x);
     if constexpr (S8) {
       uint8_t *m8 = (uint8_t *)a.m + start, *v8 = (uint8_t *)a.v + start;
-      const int64_t blk = a.block[t] + i / kBlock;
+      const int64_t blk = a.block0 + a.block[t] + i / kBlock;
       load8_f8(m8, i, n, m);
       load8_f8(v8, i, n, q);
       const float om = i < n ? a.scale_m[blk] : 0.0f, oq = i < n ? a.scale_v[blk] : 0.0f;
@@ -254,8 +254,8 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
 }
 
 template <typename T, typename G>
-hipError_t launch(const AdamArgs &a, bool s8, hipStream_t s) {
-  const dim3 grid((unsigned)a.chunk[a.n]), block(kAdamThreads);
+hipError_t launch(const AdamArgs &a, int64_t chunks, bool s8, hipStream_t s) {
+  const dim3 grid((unsigned)chunks), block(kAdamThreads);
   if (a.master && sizeof(T) == 2) {
     if (s8)
       adamw_kernel<T, G, true, true><<<grid, block, 0, s>>>(a);
@@ -333,33 +333,30 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
   int64_t at = 0, blk = 0;
   for (int t = 0; t < T;) {
     a.n = 0;
+    a.start0 = at;
+    a.block0 = blk;
     int64_t chunks = 0;
     for (; t < T && a.n < kMaxTensors; ++t) {
-      const int64_t n = tensors[t].n;
+      const int64_t n = tensors[t].n, c = (n + kChunk - 1) / kChunk;
       if (n == 0) continue;
-      const int64_t c = (n + kChunk - 1) / kChunk;
-      if (chunks + c > 0x7fffffff) {
-        if (a.n == 0) return BKMOO_EUNSUPPORTED;
-        break;
-      }
+      if (c > 0x7fffffff) return BKMOO_EUNSUPPORTED;
+      if (a.n > 0 && (chunks + c > 0x7fffffff || at + n - a.start0 > 0xffffffffll)) break;
       a.p[a.n] = tensors[t].data;
-      a.decay[a.n] = tensors[t].decay != 0;
-      a.start[a.n] = at;
-      a.block[a.n] = blk;
-      a.chunk[a.n] = (int)chunks;
+      a.start[a.n] = (uint32_t)(at - a.start0);
+      a.block[a.n] = (uint32_t)(blk - a.block0);
+      a.chunk[a.n] = (uint32_t)chunks | (tensors[t].decay != 0 ? kDecay : 0);
       at += n;
       blk += blocks_of(n);
       chunks += c;
       ++a.n;
     }
     if (a.n == 0) continue;
-    a.start[a.n] = at;
-    a.chunk[a.n] = (int)chunks;
+    a.total = at - a.start0;
     hipError_t e;
     if (dt == BKMOO_F32)
-      e = grad_dt == BKMOO_F32 ? launch<float, float>(a, s8, stream) : launch<float, __bf16>(a, s8, stream);
+      e = grad_dt == BKMOO_F32 ? launch<float, float>(a, chunks, s8, stream) : launch<float, __bf16>(a, chunks, s8, stream);
     else
-      e = grad_dt == BKMOO_F32 ? launch<__bf16, float>(a, s8, stream) : launch<__bf16, __bf16>(a, s8, stream);
+      e = grad_dt == BKMOO_F32 ? launch<__bf16, float>(a, chunks, s8, stream) : launch<__bf16, __bf16>(a, chunks, s8, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
   }
   return BKMOO_OK;
