@@ -49,7 +49,6 @@ struct AdamArgs {
   const float *grad_scale;
   float b1, c1, b2, c2, keep, step, rootc, eps;  // c = 1 - b, keep = 1 - lr wd, step = lr / (1 - b1^t)
   uint32_t seed;
-  int fine;                      // sixteen random bits a moment
   int n;                         // tensors of this launch
   int64_t start0, block0, total; // its first element in the flat vectors and block of 256, its elements
   void *p[kMaxTensors];
@@ -62,19 +61,19 @@ static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_byte __attribute__((aligned(1)));
 
-// Eight elements from i on, of n; zeros past the end.
-template <typename T>
+// Eight elements from i on, of n (all of them there if ALL); zeros past the end.
+template <bool ALL, typename T>
 __device__ __forceinline__ void load8_of(const T *p, int64_t i, int64_t n, float (&x)[8]) {
-  if (i + 8 <= n) {
+  if (ALL || i + 8 <= n) {
     load8(p + i).get(x);
     return;
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = i + e < n ? load1(p + i + e) : 0.0f;
 }
-template <typename T>
+template <bool ALL, typename T>
 __device__ __forceinline__ void store8_of(T *p, int64_t i, int64_t n, const float (&x)[8]) {
-  if (i + 8 <= n) {
+  if (ALL || i + 8 <= n) {
     store8(p + i, x);
     return;
   }
@@ -84,9 +83,10 @@ __device__ __forceinline__ void store8_of(T *p, int64_t i, int64_t n, const floa
 }
 
 // Eight e4m3 values.
+template <bool ALL>
 __device__ __forceinline__ void load8_f8(const uint8_t *p, int64_t i, int64_t n, float (&x)[8]) {
   u32x2 w = {0, 0};
-  if (i + 8 <= n) {
+  if (ALL || i + 8 <= n) {
     w = *(const u32x2_byte *)(p + i);
   } else {
 #pragma unroll
@@ -102,6 +102,7 @@ __device__ __forceinline__ void load8_f8(const uint8_t *p, int64_t i, int64_t n,
     x[4 * h + 3] = hi[1];
   }
 }
+template <bool ALL>
 __device__ __forceinline__ void store8_f8(uint8_t *p, int64_t i, int64_t n, const float (&x)[8]) {
   u32x2 w;
 #pragma unroll
@@ -110,7 +111,7 @@ __device__ __forceinline__ void store8_f8(uint8_t *p, int64_t i, int64_t n, cons
     t = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * h + 2], x[4 * h + 3], t, true);
     w[h] = (uint32_t)t;
   }
-  if (i + 8 <= n) {
+  if (ALL || i + 8 <= n) {
     *(u32x2_byte *)(p + i) = w;
     return;
   }
@@ -119,11 +120,19 @@ __device__ __forceinline__ void store8_f8(uint8_t *p, int64_t i, int64_t n, cons
     if (i + e < n) p[i + e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
 }
 
-// Maximum over the 32 lanes that hold a block.
+// Maximum over the 32 lanes that hold a block: neighbours, then the halves of 16 lanes, then
+// two rows of 16.
+template <int CTRL>
+__device__ __forceinline__ float max_dpp(float x) {
+  return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true)));
+}
 __device__ __forceinline__ float block_max(float x) {
-#pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 32));
-  return x;
+  x = max_dpp<0xB1>(x);   // lanes 1 0 3 2
+  x = max_dpp<0x4E>(x);   // lanes 2 3 0 1
+  x = max_dpp<0x141>(x);  // half rows of 16 mirrored
+  x = max_dpp<0x140>(x);  // rows mirrored
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // 32 random bits for the `number`-th element or pair of elements.
@@ -135,17 +144,117 @@ __device__ __forceinline__ uint32_t random_bits(uint32_t number, uint32_t seed) 
   return h ^ (h >> 16);
 }
 
-// 0 <= y <= 448 to one of the two e4m3 values around it: adding a random number to
+// 0 <= y <= 448 (and a rounding) to one of the two e4m3 values around it: adding a random number to
 // the 20 bits below e4m3's last place and cutting them off.  Below 2^-6 values are
 // 2^-9 apart, as they are in [2^-6, 2^-5): shifted there and back.
 __device__ __forceinline__ float round_f8(float y, uint32_t random20) {
   const float low = y < 0.015625f ? 0.015625f : 0.0f;
   const uint32_t b = (__float_as_uint(y + low) + random20) & 0xfff00000u;
-  return fminf(__uint_as_float(b) - low, kF8Max);
+  return __uint_as_float(b) - low;
 }
 
-// T: parameter, G: gradient, S8: moments in 8 bits, MASTER: a 32-bit copy takes the step.
-template <typename T, typename G, bool S8, bool MASTER>
+// Eight elements of a lane, from i on.  T: parameter, G: gradient, S8: moments in 8 bits, FINE:
+// sixteen random bits a moment, MASTER: a 32-bit copy takes the step, ALL: all eight are there (and,
+// S8, all of the block's).
+template <typename T, typename G, bool S8, bool FINE, bool MASTER, bool ALL>
+__device__ __forceinline__ void step8(const AdamArgs &a, T *p, const G *grad, float *master, int64_t start,
+                                      int64_t block, int64_t i, int64_t n, float gs, float keep) {
+  float g[8], m[8], q[8], x[8];
+  load8_of<ALL>(grad, i, n, g);
+  if constexpr (MASTER)
+    load8_of<ALL>(master, i, n, x);
+  else
+    load8_of<ALL>((const T *)p, i, n, x);
+  if constexpr (S8) {
+    uint8_t *m8 = (uint8_t *)a.m + start, *v8 = (uint8_t *)a.v + start;
+    const int64_t blk = block + i / kBlock;
+    load8_f8<ALL>(m8, i, n, m);
+    load8_f8<ALL>(v8, i, n, q);
+    const float om = ALL || i < n ? a.scale_m[blk] : 0.0f, oq = ALL || i < n ? a.scale_v[blk] : 0.0f;
+    float tm = 0.0f, tq = 0.0f, odd = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float ge = g[e] * gs;
+      m[e] = m[e] * om * a.b1 + a.c1 * ge;
+      const float r = q[e] * oq;
+      q[e] = sqrtf(r * r * a.b2 + a.c2 * ge * ge);
+      tm = fmaxf(tm, fabsf(m[e]));
+      tq = fmaxf(tq, q[e]);
+      odd += m[e] + q[e];
+    }
+    tm = block_max(tm);
+    tq = block_max(tq);
+    const float im = tm >= kTiny ? 1.0f / tm * kF8Max : 0.0f, iq = tq >= kTiny ? 1.0f / tq * kF8Max : 0.0f;
+    float wm[8], wq[8];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const uint32_t number = (uint32_t)blk * kBlock + ((uint32_t)i & (kBlock - 1)) + e;
+      uint32_t rm[2], rr[2];
+      if constexpr (FINE) {
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          const uint32_t h = random_bits(number + f, a.seed);
+          rm[f] = ((h & 0xffff) << 4) + 8;
+          rr[f] = ((h >> 16) << 4) + 8;
+        }
+      } else {
+        const uint32_t h = random_bits(number / 2, a.seed);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          rm[f] = (((h >> (16 * f)) & 255) << 12) + 2048;
+          rr[f] = (((h >> (16 * f + 8)) & 255) << 12) + 2048;
+        }
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const float xm = m[e + f] * im, xq = q[e + f] * iq;
+        wm[e + f] = copysignf(round_f8(fabsf(xm), rm[f]), xm);
+        wq[e + f] = fmaxf(round_f8(xq, rr[f]), xq > 0.0f ? 0.001953125f : 0.0f);
+      }
+    }
+    // a NaN or an infinity among them (or an overflow of the sum: nothing changes then)
+    if (!(fabsf(odd) < __builtin_inff())) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float xm = m[e] * im, xq = q[e] * iq;
+        if (!(xm == xm)) wm[e] = xm;
+        if (!(xq == xq)) wq[e] = xq;
+      }
+    }
+    if (ALL || i < n) {
+      store8_f8<ALL>(m8, i, n, wm);
+      store8_f8<ALL>(v8, i, n, wq);
+      if ((threadIdx.x & 31) == 0) {
+        a.scale_m[blk] = tm >= kTiny ? tm * (1.0f / kF8Max) : 0.0f;
+        a.scale_v[blk] = tq >= kTiny ? tq * (1.0f / kF8Max) : 0.0f;
+      }
+    }
+  } else {
+    float *m32 = (float *)a.m + start, *v32 = (float *)a.v + start;
+    load8_of<ALL>(m32, i, n, m);
+    load8_of<ALL>(v32, i, n, q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float ge = g[e] * gs;
+      m[e] = a.b1 * m[e] + a.c1 * ge;
+      q[e] = a.b2 * q[e] + a.c2 * (ge * ge);
+    }
+    store8_of<ALL>(m32, i, n, m);
+    store8_of<ALL>(v32, i, n, q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = sqrtf(q[e]);
+  }
+  // (the reciprocal instruction is within an ulp; the step it scales is added to the parameter)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = x[e] * keep - a.step * m[e] * __builtin_amdgcn_rcpf(q[e] * a.rootc + a.eps);
+  if (ALL || i < n) {
+    if constexpr (MASTER) store8_of<ALL>(master, i, n, x);
+    store8_of<ALL>(p, i, n, x);
+  }
+}
+
+// A workgroup: one chunk of one tensor.
+template <typename T, typename G, bool S8, bool FINE, bool MASTER>
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   int t = 0;
   {
@@ -157,116 +266,39 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   }
   const int64_t first = (int64_t)(blockIdx.x - (a.chunk[t] & ~kDecay)) * kChunk;
   const int64_t start = a.start0 + a.start[t], n = (t + 1 < a.n ? (int64_t)a.start[t + 1] : a.total) - a.start[t];
-  const int64_t end = first + kChunk < n ? first + kChunk : n;
+  const int64_t end = first + kChunk < n ? first + kChunk : n, block = a.block0 + a.block[t];
   T *p = (T *)a.p[t];
   const G *grad = (const G *)a.grad + start;
   float *master = MASTER ? a.master + start : nullptr;
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const float keep = a.chunk[t] & kDecay ? a.keep : 1.0f;
-  for (int64_t base = first; base < end; base += kAdamThreads * kLaneElems) {
-    const int64_t i = base + threadIdx.x * kLaneElems;
-    if (!S8 && i >= n) break;
-    float g[8], m[8], q[8], x[8];
-    load8_of(grad, i, n, g);
-    if constexpr (MASTER)
-      load8_of(master, i, n, x);
-    else
-      load8_of((const T *)p, i, n, x);
-    if constexpr (S8) {
-      uint8_t *m8 = (uint8_t *)a.m + start, *v8 = (uint8_t *)a.v + start;
-      const int64_t blk = a.block0 + a.block[t] + i / kBlock;
-      load8_f8(m8, i, n, m);
-      load8_f8(v8, i, n, q);
-      const float om = i < n ? a.scale_m[blk] : 0.0f, oq = i < n ? a.scale_v[blk] : 0.0f;
-      float tm = 0.0f, tq = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float ge = g[e] * gs;
-        m[e] = m[e] * om * a.b1 + a.c1 * ge;
-        const float r = q[e] * oq;
-        q[e] = sqrtf(r * r * a.b2 + a.c2 * ge * ge);
-        tm = fmaxf(tm, fabsf(m[e]));
-        tq = fmaxf(tq, q[e]);
-      }
-      tm = block_max(tm);
-      tq = block_max(tq);
-      const float im = tm >= kTiny ? 1.0f / tm * kF8Max : 0.0f, iq = tq >= kTiny ? 1.0f / tq * kF8Max : 0.0f;
-      float wm[8], wq[8];
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const uint32_t number = (uint32_t)blk * kBlock + ((uint32_t)i & (kBlock - 1)) + e;
-        uint32_t h[2], rm[2], rr[2];
-        if (a.fine) {
-#pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            h[f] = random_bits(number + f, a.seed);
-            rm[f] = ((h[f] & 0xffff) << 4) + 8;
-            rr[f] = ((h[f] >> 16) << 4) + 8;
-          }
-        } else {
-          h[0] = random_bits(number / 2, a.seed);
-#pragma unroll
-          for (int f = 0; f < 2; ++f) {
-            rm[f] = (((h[0] >> (16 * f)) & 255) << 12) + 2048;
-            rr[f] = (((h[0] >> (16 * f + 8)) & 255) << 12) + 2048;
-          }
-        }
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const float xm = m[e + f] * im, xq = q[e + f] * iq;
-          wm[e + f] = copysignf(round_f8(fabsf(xm), rm[f]), xm);
-          const float rq = round_f8(xq, rr[f]);
-          wq[e + f] = xq > 0.0f ? fmaxf(rq, 0.001953125f) : rq;
-          if (!(xm == xm)) wm[e + f] = xm;
-          if (!(xq == xq)) wq[e + f] = xq;
-        }
-      }
-      if (i < n) {
-        store8_f8(m8, i, n, wm);
-        store8_f8(v8, i, n, wq);
-        if ((threadIdx.x & 31) == 0) {
-          a.scale_m[blk] = tm >= kTiny ? tm * (1.0f / kF8Max) : 0.0f;
-          a.scale_v[blk] = tq >= kTiny ? tq * (1.0f / kF8Max) : 0.0f;
-        }
-      }
-    } else {
-      float *m32 = (float *)a.m + start, *v32 = (float *)a.v + start;
-      load8_of(m32, i, n, m);
-      load8_of(v32, i, n, q);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float ge = g[e] * gs;
-        m[e] = a.b1 * m[e] + a.c1 * ge;
-        q[e] = a.b2 * q[e] + a.c2 * (ge * ge);
-      }
-      store8_of(m32, i, n, m);
-      store8_of(v32, i, n, q);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) q[e] = sqrtf(q[e]);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = x[e] * keep - a.step * m[e] / (q[e] * a.rootc + a.eps);
-    if (i < n) {
-      if constexpr (MASTER) store8_of(master, i, n, x);
-      store8_of(p, i, n, x);
-    }
-  }
+  constexpr int kRound = kAdamThreads * kLaneElems;
+  const int64_t lane = (int64_t)threadIdx.x * kLaneElems;
+  int64_t base = first;
+  for (; base + kRound <= end; base += kRound)
+    step8<T, G, S8, FINE, MASTER, true>(a, p, grad, master, start, block, base + lane, n, gs, keep);
+  if (base < end && (S8 || base + lane < n))  // (S8: a block's lanes stay together)
+    step8<T, G, S8, FINE, MASTER, false>(a, p, grad, master, start, block, base + lane, n, gs, keep);
 }
 
+template <typename T, typename G, bool MASTER>
+void launch_states(const AdamArgs &a, unsigned chunks, bool s8, bool fine, hipStream_t s) {
+  if (!s8)
+    adamw_kernel<T, G, false, false, MASTER><<<chunks, kAdamThreads, 0, s>>>(a);
+  else if (fine)
+    adamw_kernel<T, G, true, true, MASTER><<<chunks, kAdamThreads, 0, s>>>(a);
+  else
+    adamw_kernel<T, G, true, false, MASTER><<<chunks, kAdamThreads, 0, s>>>(a);
+}
 template <typename T, typename G>
-hipError_t launch(const AdamArgs &a, int64_t chunks, bool s8, hipStream_t s) {
-  const dim3 grid((unsigned)chunks), block(kAdamThreads);
-  if (a.master && sizeof(T) == 2) {
-    if (s8)
-      adamw_kernel<T, G, true, true><<<grid, block, 0, s>>>(a);
-    else
-      adamw_kernel<T, G, false, true><<<grid, block, 0, s>>>(a);
-  } else {
-    if (s8)
-      adamw_kernel<T, G, true, false><<<grid, block, 0, s>>>(a);
-    else
-      adamw_kernel<T, G, false, false><<<grid, block, 0, s>>>(a);
+hipError_t launch(const AdamArgs &a, int64_t chunks, bool s8, bool fine, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (a.master) {
+      launch_states<T, G, true>(a, (unsigned)chunks, s8, fine, s);
+      return hipGetLastError();
+    }
   }
+  launch_states<T, G, false>(a, (unsigned)chunks, s8, fine, s);
   return hipGetLastError();
 }
 
@@ -329,7 +361,7 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
   a.rootc = (float)(1.0 / sqrt(1.0 - pow(hp->beta2, (double)hp->step)));
   a.eps = (float)hp->eps;
   a.seed = hp->seed;
-  a.fine = hp->beta1 > kFineBeta || hp->beta2 > kFineBeta;
+  const bool fine = hp->beta1 > kFineBeta || hp->beta2 > kFineBeta;
   int64_t at = 0, blk = 0;
   for (int t = 0; t < T;) {
     a.n = 0;
@@ -354,9 +386,9 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
     a.total = at - a.start0;
     hipError_t e;
     if (dt == BKMOO_F32)
-      e = grad_dt == BKMOO_F32 ? launch<float, float>(a, chunks, s8, stream) : launch<float, __bf16>(a, chunks, s8, stream);
+      e = grad_dt == BKMOO_F32 ? launch<float, float>(a, chunks, s8, fine, stream) : launch<float, __bf16>(a, chunks, s8, fine, stream);
     else
-      e = grad_dt == BKMOO_F32 ? launch<__bf16, float>(a, chunks, s8, stream) : launch<__bf16, __bf16>(a, chunks, s8, stream);
+      e = grad_dt == BKMOO_F32 ? launch<__bf16, float>(a, chunks, s8, fine, stream) : launch<__bf16, __bf16>(a, chunks, s8, fine, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
   }
   return BKMOO_OK;

@@ -207,6 +207,35 @@ def test_non_finite_gradient_stays_in_its_block(gpu_lib):
         assert (~torch.isfinite(p)).nonzero().view(-1).tolist() == [300]
 
 
+def test_non_finite_states_stay(gpu_lib):
+    """A step with a finite gradient does not make a non-finite moment finite again."""
+    m8 = torch.zeros(512, device="cuda")
+    m8[7] = float("nan")
+    m8, q8 = m8.to(torch.float8_e4m3fn), torch.ones(512, device="cuda")
+    q8[9] = float("nan")
+    q8 = q8.to(torch.float8_e4m3fn)
+    scales = torch.full((2, 2), 0.01, device="cuda")
+    p = torch.ones(512, device="cuda")
+    gpu_lib.adamw(gpu_lib.adamw_table([p]), torch.ones(512, device="cuda"), m8, q8, step=2, lr=0.1, scales=scales)
+    assert (~torch.isfinite(m8.float())).nonzero().view(-1).tolist() == [7]
+    assert (~torch.isfinite(q8.float())).nonzero().view(-1).tolist() == [9]
+    assert (~torch.isfinite(p)).nonzero().view(-1).tolist() == [7, 9]
+
+
+def test_many_tensors(gpu_lib):
+    """More tensors than a launch takes, empty ones among them, each with decay or not."""
+    sizes = [(i * 37) % 300 for i in range(700)]
+    p, g, m, v = make(sizes, torch.float32, torch.float32, seed=2)
+    decay = [i % 3 == 0 for i in range(len(sizes))]
+    params = [t.clone().cuda() for t in torch.split(p, sizes)]
+    want = reference(p.double(), g.double(), m.double(), v.double(), sizes, decay, 5)
+    gm, gv = m.cuda(), v.cuda()
+    gpu_lib.adamw(gpu_lib.adamw_table(params, decay), g.cuda(), gm, gv, step=5, **HP)
+    got = torch.cat([t.reshape(-1) for t in params])
+    assert off_terms(got, want[0], step_terms(p, g, m, v, 5)) <= 8 * 2.0 ** -24
+    assert off_terms(gm, want[1], terms(g, m)) <= 8 * 2.0 ** -24
+
+
 def test_views_at_odd_places_and_repeatable(gpu_lib):
     """Parameters, gradient and states that start at odd elements of larger buffers; what lies
     between them stays; a second run from the same state gives the same bits; another stream."""

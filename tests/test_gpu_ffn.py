@@ -35,7 +35,7 @@ def wide(t):
     return {k: v.double() for k, v in t.items()}
 
 
-SHAPES = [(1, 1, 1), (1, 64, 200), (1, 2048, 512), (2, 72, 136), (3, 7, 5), (16, 256, 384), (17, 256, 384), (24, 520, 264),
+SHAPES = [(1, 1, 1), (1, 64, 200), (1, 2048, 512), (2, 72, 136), (3, 7, 5), (8, 130, 258), (9, 130, 258), (16, 256, 384), (17, 256, 384), (24, 520, 264),
           (33, 128, 320), (64, 512, 96), (65, 512, 96), (130, 65, 131), (100, 1000, 72), (257, 136, 520), (300, 258, 514),
           (513, 768, 640), (1030, 264, 1000)]
 
