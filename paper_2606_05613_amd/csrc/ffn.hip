@@ -47,7 +47,7 @@ Plan plan(int dt, Mode mode, int64_t M, int64_t N, int64_t K, int64_t problems, 
       if (splits > 1 && mode != kDown && mode != kInputGrad) break;
       const int64_t tiles = ((M + side - 1) / side) * ((N + side - 1) / side) * problems * splits;
       double us = product_us(side, dt, mode, tiles, (steps + splits - 1) / splits, aligned);
-      if (splits > 1) us += 4.0 + 1.2e-6 * splits * M * N;  // written and read again, a launch
+      if (splits > 1) us += 4.0 + 1.5e-6 * splits * M * N;  // written and read again, a launch
       if (least == 0.0 || us < least) {
         least = us;
         best = Plan{side, splits};

@@ -166,7 +166,7 @@ __device__ __forceinline__ void eight_columns(f32x4 a, f32x4 b, float (&x)[8]) {
 // numbers cover patches of kPatch rows of tiles, so that the tiles in flight on
 // an XCD share rows of A and of B in its L2.
 constexpr int kXcds = 8;
-constexpr int kPatch = 4;
+constexpr int kPatch = 8;
 __device__ __forceinline__ int xcd_order(int id, int n) {
   const int q = n / kXcds, r = n % kXcds, x = id % kXcds;
   return x * q + (x < r ? x : r) + id / kXcds;
