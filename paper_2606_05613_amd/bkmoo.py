@@ -448,13 +448,13 @@ def set_wait_limit(polls: int):
 # ----------------------------------------------------------------------------
 
 
-def _ptr(t: Optional[torch.Tensor], shape, like: torch.Tensor, what: str):
-    """Pointer of a contiguous tensor of `like`'s type and device; None stays None."""
+def _ptr(t: Optional[torch.Tensor], shape, dtype, index: int, what: str):
+    """Pointer of a contiguous tensor of this shape and type on GPU `index`; None stays None."""
     if t is None:
         return None
-    if t.dtype is like.dtype and t.shape == shape and t.is_contiguous() and t.get_device() == like.get_device():
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
         return t.data_ptr()
-    raise ValueError(f"{what} must be a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}")
+    raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}")
 
 
 # the current stream's handle by device number, without a Stream object around it (2.5 us a call)
@@ -462,25 +462,27 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _run(fn, what: str, dev, *args):
-    """fn(*args, stream) with the inputs' device current."""
-    stream = _raw_stream(dev.index)
-    if torch.cuda.current_device() == dev.index:
+def _run(fn, what: str, index: int, *args):
+    """fn(*args, stream) with GPU `index`, the inputs', current."""
+    stream = _raw_stream(index)
+    if torch.cuda.current_device() == index:
         st = fn(*args, stream)
     else:
-        with torch.cuda.device(dev):
+        with torch.cuda.device(index):
             st = fn(*args, stream)
     if st != 0:
         _check(st, what)
 
 
 def _matrix(t: torch.Tensor, what: str):
-    """Rows, columns and dtype code of a 2-D GPU tensor."""
-    code = _dt(t)
-    _gpu(t, what)
-    if t.dim() != 2:
+    """Rows, columns, dtype code, dtype and GPU number of a 2-D GPU tensor."""
+    dtype, shape = t.dtype, t.shape
+    code = BF16 if dtype is torch.bfloat16 else _dt(t)
+    if not t.is_cuda:
+        _gpu(t, what)
+    if len(shape) != 2:
         raise ValueError(f"{what} must have two dimensions")
-    return t.shape[0], t.shape[1], code
+    return shape[0], shape[1], code, dtype, t.get_device()
 
 
 def _byte_workspace(ws: Optional[torch.Tensor], need: int, dev) -> torch.Tensor:
@@ -524,16 +526,16 @@ def residual_norm_forward(resid: torch.Tensor, y: torch.Tensor, weight: torch.Te
     """The norm after a block (with post_weight), its gate and residual scale, and the
     norm before the next: (resid + scale * gate * norm(y), norm of that), both [M, D].
     resid_out may be resid."""
-    M, D, dt = _matrix(resid, "resid")
-    dev, shape, vec = resid.device, resid.shape, (D,)
+    M, D, code, dt, gpu = _matrix(resid, "resid")
+    shape, vec = resid.shape, (D,)
     if resid_out is None:
         resid_out = torch.empty_like(resid, memory_format=torch.contiguous_format)
     if normed is None:
         normed = torch.empty_like(resid, memory_format=torch.contiguous_format)
-    args = (_ptr(resid, shape, resid, "resid"), _ptr(y, shape, resid, "y"), _ptr(weight, vec, resid, "weight"),
-            _ptr(post_weight, vec, resid, "post_weight"), _ptr(gate, vec, resid, "gate"), scale, eps,
-            _ptr(resid_out, shape, resid, "resid_out"), _ptr(normed, shape, resid, "normed"))
-    _run(_lib.bkmoo_residual_norm_forward, "bkmoo_residual_norm_forward", dev, M, D, dt, *args)
+    _run(_lib.bkmoo_residual_norm_forward, "bkmoo_residual_norm_forward", gpu, M, D, code,
+         _ptr(resid, shape, dt, gpu, "resid"), _ptr(y, shape, dt, gpu, "y"), _ptr(weight, vec, dt, gpu, "weight"),
+         _ptr(post_weight, vec, dt, gpu, "post_weight"), _ptr(gate, vec, dt, gpu, "gate"), scale, eps,
+         _ptr(resid_out, shape, dt, gpu, "resid_out"), _ptr(normed, shape, dt, gpu, "normed"))
     return resid_out, normed
 
 
@@ -547,24 +549,26 @@ def residual_norm_backward(dresid_out: Optional[torch.Tensor], dnormed: torch.Te
     """Gradients of residual_norm_forward: returns (dresid, dy) and writes the K tasks'
     weight gradients to dweight, dpost_weight and dgate, [K, D] with contiguous rows
     (columns of the gradient buffer).  task_rows: K + 1 offsets of the tasks' rows."""
-    M, D, dt = _matrix(resid_out, "resid_out")
-    dev, shape, vec, like = resid_out.device, resid_out.shape, (D,), resid_out
+    M, D, code, dt, gpu = _matrix(resid_out, "resid_out")
+    shape, vec = resid_out.shape, (D,)
     rows, K = _task_rows(task_rows, M)
     if dweight is None:
         raise ValueError("dweight is needed")
-    ptrs, stride = _task_grads(((dweight, "dweight"), (dpost_weight, "dpost_weight"), (dgate, "dgate")), K, D, like)
+    ptrs, stride = _task_grads(((dweight, "dweight"), (dpost_weight, "dpost_weight"), (dgate, "dgate")), K, D,
+                               resid_out)
     if dresid is None:
         dresid = torch.empty_like(resid_out, memory_format=torch.contiguous_format)
     if dy is None:
         dy = torch.empty_like(resid_out, memory_format=torch.contiguous_format)
     need = ctypes.c_size_t(0)
     _check(_lib.bkmoo_residual_norm_workspace_size(M, D, K, ctypes.byref(need)), "bkmoo_residual_norm_workspace_size")
-    ws = _byte_workspace(workspace, need.value, dev)
-    args = (_ptr(dresid_out, shape, like, "dresid_out"), _ptr(dnormed, shape, like, "dnormed"),
-            _ptr(resid_out, shape, like, "resid_out"), _ptr(y, shape, like, "y"), _ptr(weight, vec, like, "weight"),
-            _ptr(post_weight, vec, like, "post_weight"), _ptr(gate, vec, like, "gate"), scale, eps,
-            _ptr(dresid, shape, like, "dresid"), _ptr(dy, shape, like, "dy"), *ptrs, stride)
-    _run(_lib.bkmoo_residual_norm_backward, "bkmoo_residual_norm_backward", dev, M, D, dt, K, rows, *args,
+    ws = _byte_workspace(workspace, need.value, resid_out.device)
+    args = (_ptr(dresid_out, shape, dt, gpu, "dresid_out"), _ptr(dnormed, shape, dt, gpu, "dnormed"),
+            _ptr(resid_out, shape, dt, gpu, "resid_out"), _ptr(y, shape, dt, gpu, "y"),
+            _ptr(weight, vec, dt, gpu, "weight"), _ptr(post_weight, vec, dt, gpu, "post_weight"),
+            _ptr(gate, vec, dt, gpu, "gate"), scale, eps, _ptr(dresid, shape, dt, gpu, "dresid"),
+            _ptr(dy, shape, dt, gpu, "dy"), *ptrs, stride)
+    _run(_lib.bkmoo_residual_norm_backward, "bkmoo_residual_norm_backward", gpu, M, D, code, K, rows, *args,
          ws.data_ptr(), ws.numel())
     return dresid, dy
 
@@ -582,21 +586,22 @@ def ffn_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_dow
     """Gated feed-forward block: (y, u, v) with y = (act(u) * v) w_down^T, u = x w_gate^T,
     v = x w_up^T for x [M, D], w_gate and w_up [F, D], w_down [D, F].  u and v, which
     the backward pass needs, are None unless `save` is set or they are given."""
-    M, D, dt = _matrix(x, "x")
+    M, D, code, dt, gpu = _matrix(x, "x")
     if w_gate.dim() != 2:
         raise ValueError("w_gate must have two dimensions")
     F, dev = w_gate.shape[0], x.device
+    md, mf, fd, df = (M, D), (M, F), (F, D), (D, F)
     if out is None:
-        out = torch.empty((M, D), dtype=x.dtype, device=dev)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     if save and gate_out is None:
-        gate_out = torch.empty((M, F), dtype=x.dtype, device=dev)
+        gate_out = torch.empty(mf, dtype=dt, device=dev)
     if save and up_out is None:
-        up_out = torch.empty((M, F), dtype=x.dtype, device=dev)
-    ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, dt), dev)
-    args = (_ptr(x, (M, D), x, "x"), _ptr(w_gate, (F, D), x, "w_gate"), _ptr(w_up, (F, D), x, "w_up"),
-            _ptr(w_down, (D, F), x, "w_down"), _ptr(out, (M, D), x, "out"), _ptr(gate_out, (M, F), x, "gate_out"),
-            _ptr(up_out, (M, F), x, "up_out"))
-    _run(_lib.bkmoo_ffn_forward, "bkmoo_ffn_forward", dev, M, D, F, dt, ACTS[act], *args, ws.data_ptr(), ws.numel())
+        up_out = torch.empty(mf, dtype=dt, device=dev)
+    ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, code), dev)
+    _run(_lib.bkmoo_ffn_forward, "bkmoo_ffn_forward", gpu, M, D, F, code, ACTS[act], _ptr(x, md, dt, gpu, "x"),
+         _ptr(w_gate, fd, dt, gpu, "w_gate"), _ptr(w_up, fd, dt, gpu, "w_up"), _ptr(w_down, df, dt, gpu, "w_down"),
+         _ptr(out, md, dt, gpu, "out"), _ptr(gate_out, mf, dt, gpu, "gate_out"), _ptr(up_out, mf, dt, gpu, "up_out"),
+         ws.data_ptr(), ws.numel())
     return out, gate_out, up_out
 
 
@@ -609,21 +614,23 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate_out: torch.Tensor, up_o
     dw_gate, dw_up and dw_down, each [K, D * F] with contiguous rows (columns of the
     gradient buffer; a row is the flattened matrix).  task_rows: K + 1 offsets of the
     tasks' rows in the batch."""
-    M, D, dt = _matrix(x, "x")
+    M, D, code, dt, gpu = _matrix(x, "x")
     if w_gate.dim() != 2:
         raise ValueError("w_gate must have two dimensions")
-    F, dev = w_gate.shape[0], x.device
+    F = w_gate.shape[0]
+    md, mf, fd, df = (M, D), (M, F), (F, D), (D, F)
     rows, K = _task_rows(task_rows, M)
     if dw_gate is None or dw_up is None or dw_down is None:
         raise ValueError("dw_gate, dw_up and dw_down are needed")
     ptrs, stride = _task_grads(((dw_gate, "dw_gate"), (dw_up, "dw_up"), (dw_down, "dw_down")), K, D * F, x)
     if dx is None:
-        dx = torch.empty((M, D), dtype=x.dtype, device=dev)
-    ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, dt, True), dev)
-    args = (_ptr(dy, (M, D), x, "dy"), _ptr(x, (M, D), x, "x"), _ptr(gate_out, (M, F), x, "gate_out"),
-            _ptr(up_out, (M, F), x, "up_out"), _ptr(w_gate, (F, D), x, "w_gate"), _ptr(w_up, (F, D), x, "w_up"),
-            _ptr(w_down, (D, F), x, "w_down"), _ptr(dx, (M, D), x, "dx"), *ptrs, stride)
-    _run(_lib.bkmoo_ffn_backward, "bkmoo_ffn_backward", dev, M, D, F, dt, ACTS[act], K, rows, *args, ws.data_ptr(),
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, code, True), x.device)
+    args = (_ptr(dy, md, dt, gpu, "dy"), _ptr(x, md, dt, gpu, "x"), _ptr(gate_out, mf, dt, gpu, "gate_out"),
+            _ptr(up_out, mf, dt, gpu, "up_out"), _ptr(w_gate, fd, dt, gpu, "w_gate"),
+            _ptr(w_up, fd, dt, gpu, "w_up"), _ptr(w_down, df, dt, gpu, "w_down"), _ptr(dx, md, dt, gpu, "dx"), *ptrs,
+            stride)
+    _run(_lib.bkmoo_ffn_backward, "bkmoo_ffn_backward", gpu, M, D, F, code, ACTS[act], K, rows, *args, ws.data_ptr(),
          ws.numel())
     return dx
 
@@ -664,20 +671,20 @@ def adamw(table: AdamwTable, grad: torch.Tensor, moment1: torch.Tensor, moment2:
     gradients one after another (what resolve() returns).  moment1, moment2 [N]: float32, or
     float8_e4m3fn with scales float32 [2, blocks] (zeros to start with).  master: float32 [N] copy of
     bfloat16 parameters that takes the step.  grad_scale: float32 tensor of one element."""
-    dev, N = table.device, table.N
+    dev, gpu, flat = table.device, table.device.index, (table.N,)
     f8 = moment1.dtype == torch.float8_e4m3fn
     sdt = torch.float8_e4m3fn if f8 else torch.float32
-    gp = _tensor(grad, (N,), grad.dtype, dev, "grad")
-    m1, m2 = _tensor(moment1, (N,), sdt, dev, "moment1"), _tensor(moment2, (N,), sdt, dev, "moment2")
+    gp = _ptr(grad, flat, grad.dtype, gpu, "grad")
+    m1, m2 = _ptr(moment1, flat, sdt, gpu, "moment1"), _ptr(moment2, flat, sdt, gpu, "moment2")
     if f8 != (scales is not None):
         raise ValueError("scales go with 8-bit moments")
-    sc = None if scales is None else _tensor(scales, (2, table.blocks), torch.float32, dev, "scales")
-    mp = None if master is None else _tensor(master, (N,), torch.float32, dev, "master")
+    sc = _ptr(scales, (2, table.blocks), torch.float32, gpu, "scales")
+    mp = _ptr(master, flat, torch.float32, gpu, "master")
     gs = None
     if grad_scale is not None:
         if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
             raise ValueError(f"grad_scale must be one float32 value on {dev}")
         gs = grad_scale.data_ptr()
     hp = _AdamwHparams(lr, beta1, beta2, eps, weight_decay, step, seed & 0xFFFFFFFF)
-    _run(_lib.bkmoo_adamw, "bkmoo_adamw", dev, len(table.params), table.array, table.dt, N, gp, _dt(grad),
+    _run(_lib.bkmoo_adamw, "bkmoo_adamw", gpu, len(table.params), table.array, table.dt, table.N, gp, _dt(grad),
          STATE_F8 if f8 else STATE_F32, m1, m2, sc, table.blocks if f8 else 0, mp, ctypes.byref(hp), gs)
