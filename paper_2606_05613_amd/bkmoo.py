@@ -500,21 +500,21 @@ def _task_rows(task_rows: Sequence[int], M: int):
     return (ctypes.c_int64 * len(rows))(*rows), len(rows) - 1
 
 
-def _task_grads(grads, K: int, n: int, like: torch.Tensor):
+def _task_grads(grads, K: int, n: int, dtype, index: int):
     """Pointers and the common distance of the tasks' gradients: [K, n] tensors whose rows
     are contiguous (columns of the [K, N] gradient buffer), or None."""
-    stride, ptrs = None, []
+    stride, shape, ptrs = None, (K, n), []
     for t, what in grads:
         if t is None:
             ptrs.append(None)
             continue
-        if t.dtype != like.dtype or t.shape != (K, n) or t.device != like.device or (n > 1 and t.stride(1) != 1):
-            raise ValueError(f"{what} must be a {like.dtype} tensor of shape {(K, n)} with contiguous rows on "
-                             f"{like.device}")
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != index or (n > 1 and t.stride(1) != 1):
+            raise ValueError(f"{what} must be a {dtype} tensor of shape {shape} with contiguous rows on cuda:{index}")
         if K > 1:
-            if stride is not None and t.stride(0) != stride:
+            if stride is None:
+                stride = t.stride(0)
+            elif t.stride(0) != stride:
                 raise ValueError("the tasks' gradients must be equally far apart in every tensor")
-            stride = t.stride(0)
         ptrs.append(t.data_ptr())
     return ptrs, n if stride is None else stride
 
@@ -554,8 +554,8 @@ def residual_norm_backward(dresid_out: Optional[torch.Tensor], dnormed: torch.Te
     rows, K = _task_rows(task_rows, M)
     if dweight is None:
         raise ValueError("dweight is needed")
-    ptrs, stride = _task_grads(((dweight, "dweight"), (dpost_weight, "dpost_weight"), (dgate, "dgate")), K, D,
-                               resid_out)
+    ptrs, stride = _task_grads(((dweight, "dweight"), (dpost_weight, "dpost_weight"), (dgate, "dgate")), K, D, dt,
+                               gpu)
     if dresid is None:
         dresid = torch.empty_like(resid_out, memory_format=torch.contiguous_format)
     if dy is None:
@@ -622,7 +622,8 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate_out: torch.Tensor, up_o
     rows, K = _task_rows(task_rows, M)
     if dw_gate is None or dw_up is None or dw_down is None:
         raise ValueError("dw_gate, dw_up and dw_down are needed")
-    ptrs, stride = _task_grads(((dw_gate, "dw_gate"), (dw_up, "dw_up"), (dw_down, "dw_down")), K, D * F, x)
+    ptrs, stride = _task_grads(((dw_gate, "dw_gate"), (dw_up, "dw_up"), (dw_down, "dw_down")), K, D * F, dt,
+                               gpu)
     if dx is None:
         dx = torch.empty_like(x, memory_format=torch.contiguous_format)
     ws = _byte_workspace(workspace, ffn_workspace_size(M, D, F, code, True), x.device)
