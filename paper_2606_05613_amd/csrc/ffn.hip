@@ -3,6 +3,7 @@
 #include "elem.h"
 #include "ffn.h"
 #include "layer_common.h"
+#include "mfma.h"
 
 namespace bkmoo {
 
@@ -13,7 +14,7 @@ constexpr int kCus = 256;        // MI355X
 constexpr int kMaxSplits = 16;
 
 // How a product is cut: tiles of side x side, the sum over k in `splits` parts (partial sums in
-// fp32, added in order by split_sum_kernel).
+// fp32, added in order by a kernel of their own).
 struct Plan {
   int side, splits;
 };
@@ -44,7 +45,7 @@ Plan plan(int dt, Mode mode, int64_t M, int64_t N, int64_t K, int64_t problems, 
   const int64_t steps = (K * elem_bytes(dt) + 127) / 128;
   for (int side = aligned ? 256 : 128; side >= 64; side /= 2)
     for (int splits = 1; splits <= kMaxSplits && (splits == 1 || steps / splits >= 4); splits *= 2) {
-      if (splits > 1 && mode != kDown && mode != kInputGrad) break;
+      if (splits > 1 && (mode == kGateUp || mode == kWeightGrad)) break;
       const int64_t tiles = ((M + side - 1) / side) * ((N + side - 1) / side) * problems * splits;
       double us = product_us(side, dt, mode, tiles, (steps + splits - 1) / splits, aligned);
       if (splits > 1) us += 4.0 + 1.5e-6 * splits * M * N;  // written and read again, a launch
@@ -56,35 +57,98 @@ Plan plan(int dt, Mode mode, int64_t M, int64_t N, int64_t K, int64_t problems, 
   return best;
 }
 
-// Eight elements a thread: the parts in order, rounded once.
-template <typename T>
-__global__ __launch_bounds__(256) void split_sum_kernel(const float *part, int splits, int64_t n, T *out) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (i >= n) return;
+// Element i of a split sum and the seven after it: the parts in order.  Those past n stay as they are.
+__device__ __forceinline__ void add_parts(const float *part, int splits, int64_t n, int64_t i, float (&s)[8]) {
   if (i + 8 <= n) {
-    float s[8], x[8];
+    float x[8];
     load8(part + i).get(s);
     for (int k = 1; k < splits; ++k) {
       load8(part + k * n + i).get(x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[e] += x[e];
     }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (i + e < n) {
+      s[e] = part[i + e];
+      for (int k = 1; k < splits; ++k) s[e] += part[k * n + i + e];
+    }
+}
+
+// Eight elements a thread, rounded once.
+template <typename T>
+__global__ __launch_bounds__(256) void split_sum_kernel(const float *part, int splits, int64_t n, T *out) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= n) return;
+  float s[8];
+  add_parts(part, splits, n, i, s);
+  if (i + 8 <= n) {
     store8(out + i, s);
     return;
   }
-  for (int64_t j = i; j < n; ++j) {
-    float s = part[j];
-    for (int k = 1; k < splits; ++k) s += part[k * n + j];
-    out[j] = (T)s;
-  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (i + e < n) out[i + e] = (T)s[e];
 }
 
-hipError_t split_sum(int dt, const float *part, int splits, int64_t n, void *out, hipStream_t s) {
+// The same for dh, and what the hidden gradient's epilogue makes of it.  (Few rows of a wide model: F / 64 tiles
+// alone do not fill the chip.  The product whole / in parts with this kernel, us: 16 x 2048 x 6144 bf16 22.5 /
+// 9.1 + 4.3, fp32 64 / 19.6 + 5.6; 16 x 4096 x 14336 bf16 61 / 37.5 + 4.3; 200 x 2048 x 6144 fp32 88 / 63 + 8.8.)
+template <typename T>
+__global__ __launch_bounds__(256) void split_hidden_kernel(const float *part, int splits, int64_t n, int act, const T *u,
+                                                           const T *v, T *du, T *dv, T *h) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= n) return;
+  const bool whole = i + 8 <= n;
+  float d[8], xu[8], xv[8];
+  if (whole) {
+    load8(u + i).get(xu);
+    load8(v + i).get(xv);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      d[e] = 0.0f;
+      xu[e] = i + e < n ? load1(u + i + e) : 0.0f;
+      xv[e] = i + e < n ? load1(v + i + e) : 0.0f;
+    }
+  }
+  add_parts(part, splits, n, i, d);
+  float yu[8], yv[8], yh[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float a, da;
+    gate_act_grad<T>(xu[e], act, a, da);
+    yu[e] = d[e] * xv[e] * da;
+    yv[e] = d[e] * a;
+    yh[e] = a * xv[e];
+  }
+  if (whole) {
+    store8(du + i, yu);
+    store8(dv + i, yv);
+    store8(h + i, yh);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (i + e < n) {
+      du[i + e] = (T)yu[e];
+      dv[i + e] = (T)yv[e];
+      h[i + e] = (T)yh[e];
+    }
+}
+
+// What joins a split sum: the rounded result, or (kHiddenGrad) the gradients made of it.
+template <typename T>
+hipError_t join(Mode mode, const TileArgs &g, hipStream_t s) {
+  const int64_t n = g.M * g.N;
   const unsigned grid = (unsigned)((n + 2047) / 2048);
-  if (dt == F32)
-    split_sum_kernel<<<grid, 256, 0, s>>>(part, splits, n, (float *)out);
+  if (mode == kHiddenGrad)
+    split_hidden_kernel<<<grid, 256, 0, s>>>(g.partial, g.splits, n, g.act, (const T *)g.u, (const T *)g.v,
+                                             (T *)g.out[0], (T *)g.out[1], (T *)g.out[2]);
   else
-    split_sum_kernel<<<grid, 256, 0, s>>>(part, splits, n, (__bf16 *)out);
+    split_sum_kernel<<<grid, 256, 0, s>>>(g.partial, g.splits, n, (T *)g.out[0]);
   return hipGetLastError();
 }
 
@@ -99,11 +163,17 @@ FfnLayout ffn_layout(int64_t M, int64_t D, int64_t F, int dt, bool backward) {
   L.du = mf;
   L.dv = L.du + (backward ? mf : 0);
   L.partial = L.dv + (backward ? mf : 0);
-  const Mode mode = backward ? kInputGrad : kDown;
-  const int a = plan(dt, mode, M, D, backward ? 2 * F : F, 1, true).splits;
-  const int b = plan(dt, mode, M, D, backward ? 2 * F : F, 1, false).splits;
-  const int splits = a > b ? a : b;
-  L.total = L.partial + (splits > 1 ? align256((size_t)splits * M * D * sizeof(float)) : 0);
+  size_t partial = 0;
+  auto need = [&](Mode mode, int64_t N, int64_t K) {
+    for (const bool aligned : {false, true}) {
+      const int splits = plan(dt, mode, M, N, K, 1, aligned).splits;
+      const size_t bytes = splits > 1 ? align256((size_t)splits * M * N * sizeof(float)) : 0;
+      if (bytes > partial) partial = bytes;
+    }
+  };
+  need(backward ? kInputGrad : kDown, D, backward ? 2 * F : F);
+  if (backward) need(kHiddenGrad, F, D);
+  L.total = L.partial + partial;
   return L;
 }
 
@@ -113,19 +183,18 @@ bkmoo_status check_ffn(int64_t M, int64_t D, int64_t F, int dt, int act) {
   return BKMOO_OK;
 }
 
-// y = h Wd^T or dx = du Wg + dv Wu, the sum split where that fills the chip.
-hipError_t narrow_product(int dt, Mode mode, TileArgs g, int64_t M, int64_t D, int64_t F, void *out, float *partial,
-                          bool aligned, hipStream_t s) {
-  const Plan p = plan(dt, mode, M, D, mode == kInputGrad ? 2 * F : F, 1, aligned);
+// A product of one matrix [M][N], the sum over K a segment (of kInputGrad's two) split where that fills the chip.
+hipError_t product(int dt, Mode mode, TileArgs g, int64_t M, int64_t N, int64_t K, float *partial, bool aligned,
+                   hipStream_t s) {
+  const Plan p = plan(dt, mode, M, N, mode == kInputGrad ? 2 * K : K, 1, aligned);
   g.M = M;
-  g.N = D;
-  g.K = F;
-  g.out[0] = out;
+  g.N = N;
+  g.K = K;
   g.splits = p.splits;
   g.partial = partial;
-  hipError_t e = launch_ffn_tile(dt, mode, g, 1, aligned, p.side, s);
-  if (e == hipSuccess && g.splits > 1) e = split_sum(dt, partial, g.splits, M * D, out, s);
-  return e;
+  const hipError_t e = launch_ffn_tile(dt, mode, g, 1, aligned, p.side, s);
+  if (e != hipSuccess || g.splits == 1) return e;
+  return dt == F32 ? join<float>(mode, g, s) : join<__bf16>(mode, g, s);
 }
 
 }  // namespace
@@ -190,7 +259,8 @@ extern "C" bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo
   TileArgs d = {};
   d.a[0] = ws + L.h;
   d.b[0] = w_down;
-  return status_of(narrow_product(dt, kDown, d, M, D, F, y, (float *)(ws + L.partial), aligned, stream));
+  d.out[0] = y;
+  return status_of(product(dt, kDown, d, M, D, F, (float *)(ws + L.partial), aligned, stream));
 }
 
 extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, bkmoo_act act, int32_t K,
@@ -230,19 +300,16 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
     g.out[0] = du;
     g.out[1] = dv;
     g.out[2] = h;
-    g.M = M;
-    g.N = F;
-    g.K = D;
     g.act = act == BKMOO_SILU ? kSilu : kGelu;
-    g.splits = 1;
-    e = launch_ffn_tile(dt, kHiddenGrad, g, 1, aligned, plan(dt, kHiddenGrad, M, F, D, 1, aligned).side, stream);
+    e = product(dt, kHiddenGrad, g, M, F, D, (float *)(ws + L.partial), aligned, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
     TileArgs d = {};
     d.a[0] = du;
     d.a[1] = dv;
     d.b[0] = w_gate;
     d.b[1] = w_up;
-    e = narrow_product(dt, kInputGrad, d, M, D, F, dx, (float *)(ws + L.partial), aligned, stream);
+    d.out[0] = dx;
+    e = product(dt, kInputGrad, d, M, D, F, (float *)(ws + L.partial), aligned, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
   }
   TileArgs w = {};

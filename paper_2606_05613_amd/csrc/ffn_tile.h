@@ -237,6 +237,15 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
   } else if constexpr (MODE == kHiddenGrad) {
     const T *pu = (const T *)g.u, *pv = (const T *)g.v;
     T *du = (T *)g.out[0], *dv = (T *)g.out[1], *h = (T *)g.out[2];
+    if (g.splits > 1) {  // a part of dh's sum
+      float *part = g.partial + (int64_t)prob * Mo * No;
+      everywhere([&](auto all, int i, int q, int64_t at, int n) {
+        float x[8];
+        eight_columns(acc[i][2 * q], acc[i][2 * q + 1], x);
+        put(all, part + at, x, n);
+      });
+      return;
+    }
     auto finish = [&](auto all, int i, int q, int64_t at, int n, const float (&u)[8], const float (&v)[8]) {
       float d[8], xu[8], xv[8], xh[8];
       eight_columns(acc[i][2 * q], acc[i][2 * q + 1], d);
@@ -370,7 +379,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
     x.steps_seg = (int)((x.K + BK - 1) / BK);
     x.t0 = 0;
     x.t1 = x.steps_seg * (MODE == kInputGrad ? 2 : 1);
-    if constexpr (MODE == kDown || MODE == kInputGrad) {
+    if constexpr (MODE == kDown || MODE == kHiddenGrad || MODE == kInputGrad) {
       if (g.splits > 1) {
         const int per = (x.t1 + g.splits - 1) / g.splits;
         x.t0 = x.prob * per < x.t1 ? x.prob * per : x.t1;

@@ -123,6 +123,23 @@ def test_many_tasks_of_every_length(gpu_lib, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,D,F", [(1, 2048, 65), (37, 2048, 193), (66, 1025, 97)])
+def test_backward_with_split_sums(gpu_lib, M, D, F, dtype):
+    """Few rows of a wide model: the sums over D of the hidden gradient are split and joined (sizes that end inside
+    the joining kernel's eight elements, rows off four bytes)."""
+    print(f"case ffn backward split M={M} D={D} F={F} {dtype}", flush=True)
+    t = inputs(M, D, F, dtype, seed=8)
+    rows = [0, M // 2, M]
+    d, w = gpu(t), wide(t)
+    for act in ("silu", "gelu"):
+        dx, _, cut = backward(gpu_lib, d, dtype, rows, act)
+        want = ref.ffn_backward(w["dy"], w["x"], w["u"], w["v"], w["wg"], w["wu"], w["wd"], act, rows)
+        assert ref.off(dx, want[0]) <= tol(dtype, 2 * max(D, F))
+        for k in range(3):
+            assert ref.off(cut[k].reshape(want[1 + k].shape), want[1 + k]) <= tol(dtype, max(M, D))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("shift", [1, 2, 4])
 def test_unaligned_operands(gpu_lib, dtype, shift):
     """Contiguous operands that start off 16 bytes take the other loads: same results to rounding."""
