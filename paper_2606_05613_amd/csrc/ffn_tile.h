@@ -15,8 +15,8 @@
 // step t's buffer is refilled with step t + 2 and the first half of step t + 1 is read
 // while the second half of step t is multiplied: the barrier finds every wave with its
 // next operands in registers.  Rows past the end of a matrix fall outside the
-// descriptor's range and arrive as zeros; so do the chunks past K of a K-contiguous
-// operand, and a chunk that K ends in is cleaned in LDS.  (The loads need rows at
+// descriptor's range and arrive as zeros; what a K-contiguous operand's last step brings of
+// the next rows is cleared in LDS.  (The loads need rows at
 // multiples of four bytes: rows of an odd number of bf16 go through registers instead.)
 //
 // LDS layouts (16-byte chunks; the loads fill LDS in lane order, so a layout is
@@ -178,6 +178,21 @@ __device__ __forceinline__ void tile_of(int id, int tm, int tn, int &m, int &n) 
   n = (id % per) / rows;
 }
 
+// f(0), f(1), ... f(N - 1), each with its number as a constant.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void in_turn(F &&f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    in_turn<N, I + 1>(f);
+  }
+}
+// How many of `count` things spread over `places` places come before place p.
+constexpr int due(int count, int places, int p) {
+  int n = 0;
+  while (n < count && n * places / count < p) ++n;
+  return n;
+}
+
 // What becomes of a wave's sums.
 template <typename T, Mode MODE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)[BM / WM / 16][BN / WN / 16], int prob,
@@ -326,7 +341,7 @@ constexpr int kTileStores = [] {
 }();
 
 template <typename T, Mode MODE, int BM, int BN, int WM, int WN, bool ALIGNED>
-__global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArgs g) {
+__global__ __launch_bounds__(64 * WM * WN, BM * BN / (WM * WN) > 8192 ? 1 : 2) void ffn_tile_kernel(const TileArgs g) {
   constexpr int kWaves = WM * WN;
   constexpr bool AKC = MODE != kWeightGrad;
   constexpr bool BKC = MODE == kGateUp || MODE == kDown;
@@ -476,29 +491,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
   constexpr int kLoads = SA::kPer + SB::kPer;
   auto piece = [&](const Step &x, int i) {
     if (i < SA::kPer) {
-      uint32_t off = aoff[i];
-      if (AKC && x.left < BK) {
-        int row, chunk;
-        SA::place(wave * SA::kPer + i, lane, row, chunk);
-        if (chunk * (16 / ES) >= x.left) off = kNowhere;
-      }
-      load_to_lds(x.la + i * 1024, x.a, off);
+      load_to_lds(x.la + i * 1024, x.a, aoff[i]);
     } else {
       const int q = i - SA::kPer;
-      uint32_t off = boff[q];
-      if (BKC && x.left < BK) {
-        int row, chunk;
-        SB::place(wave * SB::kPer + q, lane, row, chunk);
-        if (chunk * (16 / ES) >= x.left) off = kNowhere;
-      }
-      load_to_lds(x.lb + q * 1024, SB::template second<kHalf>(wave, q) ? x.b2 : x.b, off);
+      load_to_lds(x.lb + q * 1024, SB::template second<kHalf>(wave, q) ? x.b2 : x.b, boff[q]);
     }
   };
 
-  // A step that ends inside a 16-byte chunk of its rows: what the loads brought of the next rows
-  // is cleared, by the lane that loaded it.
+  // The step that a sum ends in: what the loads brought of the next rows is cleared, by the
+  // lane that loaded it.
   auto clear = [&](const Step &x) {
-    if ((!AKC && !BKC) || x.left >= BK || x.left % (16 / ES) == 0) return;
+    if ((!AKC && !BKC) || x.left >= BK) return;
     int at = lane;
     asm volatile("" : "+v"(at));  // worked out here, once a tile: no registers for it in the loop
 #pragma unroll
@@ -512,7 +515,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
       else
         SB::place(wave * SB::kPer + q, at, row, chunk);
       const int keep = (x.left - chunk * (16 / ES)) * ES;
-      if (keep > 0 && keep < 16) keep_bytes((isa ? x.la : x.lb) + q * 1024 + at * 16, keep);
+      if (keep < 16) keep_bytes((isa ? x.la : x.lb) + q * 1024 + at * 16, keep);
     }
   };
 
@@ -552,6 +555,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
     }
   };
 
+  constexpr bool kInPlace = BM * BN / kWaves > 8192 && ES == 2;
   f32x4 acc[TM][TN];
   const int wm = wave / WN, wn = wave % WN;
   const Reader<T, BM, AKC> reada(wm * TM * 16, lane);
@@ -572,21 +576,27 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
   auto work = [&](auto half, auto loads, int buf, const Step &x) {
     constexpr int HALF = decltype(half)::value;
     constexpr bool LOAD = decltype(loads)::value;
-    constexpr int kReads = TM + TN, kEach = TM > 2 ? (kReads + TM - 3) / (TM - 2) : kReads;
-    constexpr int kLoadEach = TM > 1 ? 2 * kLoads / TM : kLoads;
+    constexpr int kReads = TM + TN, kAll = TM * TN;
+    in_turn<kAll>([&](auto at) {
+      constexpr int P = decltype(at)::value;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-#pragma unroll
-      for (int q = i * kEach; q < (i + 1) * kEach; ++q)
-        if (q < kReads) read(HALF ^ 1, buf, q);
+      for (int q = due(kReads, kAll * 3 / 4, P); q < due(kReads, kAll * 3 / 4, P + 1); ++q) read(HALF ^ 1, buf, q);
       if constexpr (LOAD)
 #pragma unroll
-        for (int q = i * kLoadEach; q < (i + 1) * kLoadEach; ++q)
-          if (q < kLoads) piece(x, q);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
+        for (int q = due(kLoads, kAll, P); q < due(kLoads, kAll, P + 1); ++q) piece(x, q);
+      constexpr int i = P / TN, j = P % TN;
+      if constexpr (kInPlace)
+        multiply_in_place(fb[HALF][j], fa[HALF][i], acc[i][j]);
+      else
+        acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
-    }
+    });
+  };
+  auto settle = [&]() {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      for (int j = 0; j < TN; j += 4)
+        asm volatile("s_nop 15" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]), "+a"(acc[i][j + 2]), "+a"(acc[i][j + 3]));
   };
   using First = std::integral_constant<int, 0>;
   using Second = std::integral_constant<int, 1>;
@@ -616,6 +626,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    if constexpr (kInPlace) settle();
     if constexpr (!ALIGNED) {
       barrier_lds();
       buf = 0;
@@ -655,6 +666,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
         put(buf);
       asm volatile("" ::: "memory");  // the reads stay in this iteration
     }
+    if constexpr (kInPlace) settle();
     stored = z.m0 + BM <= z.M && z.n0 + (GU ? BN / 2 : BN) <= z.N;
     store_tile<T, MODE, BM, BN, WM, WN>(g, acc, z.prob, z.m0, z.n0, z.M, z.N, wm, wn, lane);
   }
