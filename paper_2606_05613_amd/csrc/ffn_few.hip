@@ -7,9 +7,9 @@
 // LDS of its own that loads fill ahead: no wave waits for another before the sums meet, in
 // wave order.
 //
-// us, gate and up / down: D=2048 F=6144, one token 11.6 / 8.2 (75 MB at 3.8 TB/s), 24 tokens
-// 12.4 / 12.7; D=4096 F=14336, one 41.6 / 21.7 (352 MB at 5.6 TB/s), 24 45.1 / 27.8, 64
-// 52.6 / 42.8.  Loads straight into the matrix layout instead of LDS, which ask for 16
+// us, gate and up / down: D=2048 F=6144, one token 9.9 / 7.8 (75 MB at 4.3 TB/s), 24 tokens
+// 10.4 / 8.4; D=4096 F=14336, one 41.9 / 21.7 (352 MB at 5.5 TB/s), 24 44.9 / 27.9, 64
+// 51.9 / 42.7.  Loads straight into the matrix layout instead of LDS, which ask for 16
 // bytes of 16 rows in turn, four times the look-ups of lines: 46.3 / 22.2 and, with 24 tokens, 58.7
 // / 36.7.
 #include "elem.h"

@@ -18,7 +18,8 @@ hipError_t launch_mode(TileArgs g, int tasks, int side, hipStream_t s) {
   // As many workgroups as the chip holds at once (a CU one of the largest, two of the next or four of
   // the smallest), each with tiles to the end: a tile's first steps travel while the one before is stored
   // (M=4096, D=2048, F=6144, us, a workgroup a tile / these: gate and up 178 / 167, down 114 /
-  // 95, weight gradients 324 / 301; 8192 x 4096 x 14336: 1772 / 1749, 857 / 852, 2564 / 2525).
+  // 95, weight gradients 324 / 301; 8192 x 4096 x 14336: 1772 / 1749, 857 / 852, 2564 / 2525;
+  // with loads and reads placed by rows of pieces).
   // The hidden gradient's epilogue waits for loads of its own, which the next tile's would
   // hold up: a workgroup a tile (963 / 1079).
   const int64_t cus = MODE == kHiddenGrad ? n : device_cu_count();
