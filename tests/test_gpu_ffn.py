@@ -182,6 +182,26 @@ def test_extreme_and_non_finite_values(gpu_lib, M):
         assert ref.off(dx, want) <= tol(torch.float32, 2 * F)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M", [5, 100, 300])
+def test_rows_that_end_inside_a_step_keep_to_themselves(gpu_lib, M, dtype):
+    """Rows whose last step of the sum runs into the next row: what is there (NaN) stays out."""
+    D, F = 70, 90
+    t = inputs(M, D, F, dtype, seed=9)
+    w = wide(t)
+    for k in ("x", "dy", "u", "v"):
+        t[k][2] = float("nan")
+    d = gpu(t)
+    others = [m for m in range(M) if m != 2]
+    y = gpu_lib.ffn_forward(d["x"], d["wg"], d["wu"], d["wd"])[0]
+    dx, _, _ = backward(gpu_lib, d, dtype, [0, 2, M], "silu")
+    want = ref.ffn_forward(w["x"], w["wg"], w["wu"], w["wd"], "silu")[0]
+    grad = ref.ffn_backward(w["dy"], w["x"], w["u"], w["v"], w["wg"], w["wu"], w["wd"], "silu", [0, 2, M])[0]
+    assert bool(torch.isnan(y[2]).all()) and bool(torch.isnan(dx[2]).all())
+    assert ref.off(y[others], want[others]) <= tol(dtype, F)
+    assert ref.off(dx[others], grad[others]) <= tol(dtype, 2 * F)
+
+
 @pytest.mark.parametrize("M", [1, 20, 300])
 def test_other_stream_workspace_and_repeatable(gpu_lib, M):
     """The same bits from a caller's own (dirty) workspace on another stream; outputs may be given."""
