@@ -103,6 +103,13 @@ __device__ __forceinline__ Eight<float> load8(const float *p) {
   return {*(const u32x4_any *)p, *(const u32x4_any *)(p + 4)};
 }
 __device__ __forceinline__ Eight<__bf16> load8(const __bf16 *p) { return {*(const u32x4_any *)p}; }
+// The eight elements from c on of a row of n, zeros past its end.
+__device__ __forceinline__ Eight<float> guarded_load8(const float *row, int64_t c, int64_t n) {
+  return {guarded_chunk(row, c, n), guarded_chunk(row, c + 4, n)};
+}
+__device__ __forceinline__ Eight<__bf16> guarded_load8(const __bf16 *row, int64_t c, int64_t n) {
+  return {guarded_chunk(row, c, n)};
+}
 __device__ __forceinline__ void store8(float *p, const float (&x)[8]) {
   u32x4 a, b;
 #pragma unroll

@@ -287,45 +287,43 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
       put(all, dv + at, xv, n);
       put(all, h + at, xh, n);
     };
-    if (inside) {
-      // u and v of the next row of pieces travel while this one is worked on
-      Eight<T> nu[2][kPairs], nv[2][kPairs];
-      auto ask = [&](int i) {
+    // u and v of the next row of pieces travel while this one is worked on (past an end: of the
+    // last row or zeros)
+    Eight<T> nu[2][kPairs], nv[2][kPairs];
+    auto ask = [&](auto all, int i) {
 #pragma unroll
-        for (int q = 0; q < kPairs; ++q) {
-          const int64_t at = (mrow + i * 16) * No + nwave + q * 32;
-          nu[i & 1][q] = load8(pu + at);
-          nv[i & 1][q] = load8(pv + at);
+      for (int q = 0; q < kPairs; ++q) {
+        const int64_t m = mrow + i * 16, n = nwave + q * 32;
+        if constexpr (decltype(all)::value) {
+          nu[i & 1][q] = load8(pu + m * No + n);
+          nv[i & 1][q] = load8(pv + m * No + n);
+        } else {
+          const int64_t row = (m < Mo ? m : Mo - 1) * No;
+          nu[i & 1][q] = guarded_load8(pu + row, n, No);
+          nv[i & 1][q] = guarded_load8(pv + row, n, No);
         }
-      };
-      ask(0);
+      }
+    };
+    auto work = [&](auto all) {
+      ask(all, 0);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
-        if (i + 1 < TM) ask(i + 1);
+        if (i + 1 < TM) ask(all, i + 1);
 #pragma unroll
         for (int q = 0; q < kPairs; ++q) {
           float u[8], v[8];
           nu[i & 1][q].get(u);
           nv[i & 1][q].get(v);
-          finish(std::true_type{}, i, q, (mrow + i * 16) * No + nwave + q * 32, 8, u, v);
+          const int64_t m = mrow + i * 16, n = nwave + q * 32;
+          const int64_t left = decltype(all)::value || m < Mo ? No - n : 0;
+          finish(all, i, q, m * No + n, decltype(all)::value || left >= 8 ? 8 : left > 0 ? (int)left : 0, u, v);
         }
       }
-    } else {
-      each(std::false_type{}, [&](auto all, int i, int q, int64_t at, int n) {
-        float u[8], v[8];
-        if (n == 8) {
-          load8(pu + at).get(u);
-          load8(pv + at).get(v);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            u[e] = e < n ? load1(pu + at + e) : 0.0f;
-            v[e] = e < n ? load1(pv + at + e) : 0.0f;
-          }
-        }
-        finish(all, i, q, at, n, u, v);
-      });
-    }
+    };
+    if (inside)
+      work(std::true_type{});
+    else
+      work(std::false_type{});
   } else {
     T *out = MODE == kWeightGrad ? (T *)g.out[prob % 3] + (prob / 3) * g.task_stride : (T *)g.out[0];
     float *part = nullptr;
