@@ -344,6 +344,14 @@ __global__ __launch_bounds__(64 * WAVES *GROUPS, 2) void norm_backward_kernel(co
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int64_t c = (int64_t)(i * WAVES * 64 + at) * V;
+      if (c + V <= D) {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+          *(u32x4_any *)(part + c + e) = pack(*(const float(*)[4]) & sw[i][e]);
+          *(u32x4_any *)(part + D + c + e) = pack(*(const float(*)[4]) & ss[i][e]);
+        }
+        continue;
+      }
 #pragma unroll
       for (int e = 0; e < V; ++e)
         if (c + e < D) {
