@@ -23,9 +23,10 @@ struct Plan {
 // from times on MI355X.  bf16: a step of a tile of 256 takes a CU 1.8 us; of tiles of 128 one
 // 1.0 and two side by side 1.2, of 64 0.56 to 0.95 for one to four: small tiles lose to L2 and
 // LDS traffic, large ones to CUs without one.  fp32 is bound by the matrix cores at every
-// side.  The epilogue adds what its accesses take.  (us at 64 / 128 / 256, M x D x F: gate
-// and up 100 x 2048 x 6144 22 / 32 / 60, 1000 x 1024 x 3000 26 / 23 / 34, 512 x 4096 x 14336 240 /
-// 153 / 115; fp32 weight gradients 777 x 500 x 1364 42 / 46 / 82.)
+// side.  The epilogue adds what its accesses take, the hidden gradient's the most (us at 128
+// and 256: 3000 x 1024 x 3000 52 and 66, 4096 x 2048 x 6144 157 and 181).  (us at 64 / 128 / 256,
+// M x D x F: gate and up 100 x 2048 x 6144 22 / 32 / 60, 1000 x 1024 x 3000 26 / 23 / 34, 512 x
+// 4096 x 14336 240 / 153 / 115; fp32 weight gradients 777 x 500 x 1364 42 / 46 / 82.)
 double product_us(int side, int dt, Mode mode, int64_t tiles, int64_t steps, bool aligned) {
   const int64_t t = (tiles + kCus - 1) / kCus;  // of the busiest CU
   static const double four[4] = {0.0, 0.56, 0.65, 0.8};
@@ -35,7 +36,8 @@ double product_us(int side, int dt, Mode mode, int64_t tiles, int64_t steps, boo
   else
     step = side == 256 ? 1.8 * t : side == 128 ? 1.2 * (t / 2) + 1.0 * (t % 2) : 0.95 * (t / 4) + four[t % 4];
   if (!aligned) step *= 1.5;
-  const double end = (side == 256 ? 8.0 : side == 128 ? 2.5 : 1.0) * (mode == kHiddenGrad ? 3.0 : 1.0);
+  const double end = mode != kHiddenGrad ? (side == 256 ? 8.0 : side == 128 ? 2.5 : 1.0)
+                                         : (side == 256 ? 36.0 : side == 128 ? 7.5 : 3.0);
   return steps * step + t * end;
 }
 
