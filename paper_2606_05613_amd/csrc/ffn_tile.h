@@ -350,7 +350,7 @@ constexpr int kTileStores = [] {
 }();
 
 template <typename T, Mode MODE, int BM, int BN, int WM, int WN, bool ALIGNED>
-__global__ __launch_bounds__(64 * WM * WN, BM * BN / (WM * WN) > 8192 ? 1 : 2) void ffn_tile_kernel(const TileArgs g) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArgs g) {
   constexpr int kWaves = WM * WN;
   constexpr bool AKC = MODE != kWeightGrad;
   constexpr bool BKC = MODE == kGateUp || MODE == kDown;
@@ -564,7 +564,6 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN / (WM * WN) > 8192 ? 1 : 2) v
     }
   };
 
-  constexpr bool kInPlace = BM * BN / kWaves > 8192 && ES == 2;
   f32x4 acc[TM][TN];
   const int wm = wave / WN, wn = wave % WN;
   const Reader<T, BM, AKC> reada(wm * TM * 16, lane);
@@ -594,18 +593,9 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN / (WM * WN) > 8192 ? 1 : 2) v
 #pragma unroll
         for (int q = due(kLoads, kAll, P); q < due(kLoads, kAll, P + 1); ++q) piece(x, q);
       constexpr int i = P / TN, j = P % TN;
-      if constexpr (kInPlace)
-        multiply_in_place(fb[HALF][j], fa[HALF][i], acc[i][j]);
-      else
-        acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
+      acc[i][j] = multiply(fb[HALF][j], fa[HALF][i], acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
     });
-  };
-  auto settle = [&]() {
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-      for (int j = 0; j < TN; j += 4)
-        asm volatile("s_nop 15" : "+a"(acc[i][j]), "+a"(acc[i][j + 1]), "+a"(acc[i][j + 2]), "+a"(acc[i][j + 3]));
   };
   using First = std::integral_constant<int, 0>;
   using Second = std::integral_constant<int, 1>;
@@ -635,7 +625,6 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN / (WM * WN) > 8192 ? 1 : 2) v
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    if constexpr (kInPlace) settle();
     if constexpr (!ALIGNED) {
       barrier_lds();
       buf = 0;
@@ -675,7 +664,6 @@ __global__ __launch_bounds__(64 * WM * WN, BM * BN / (WM * WN) > 8192 ? 1 : 2) v
         put(buf);
       asm volatile("" ::: "memory");  // the reads stay in this iteration
     }
-    if constexpr (kInPlace) settle();
     stored = z.m0 + BM <= z.M && z.n0 + (GU ? BN / 2 : BN) <= z.N;
     store_tile<T, MODE, BM, BN, WM, WN>(g, acc, z.prob, z.m0, z.n0, z.M, z.N, wm, wn, lane);
   }

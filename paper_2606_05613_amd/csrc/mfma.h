@@ -82,10 +82,6 @@ __device__ __forceinline__ f32x4 multiply(const Frag<float> &n, const Frag<float
   return acc;
 }
 
-__device__ __forceinline__ void multiply_in_place(const Frag<__bf16> &n, const Frag<__bf16> &m, f32x4 &acc) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(n.v), "v"(m.v));
-}
-
 // Gate activation and its derivative: z s(z') with the logistic function s (GELU's tanh
 // form is u times s of twice tanh's argument).  One exponential of a non-positive
 // number gives s and 1 - s without cancellation.  bf16: the exponential and reciprocal
