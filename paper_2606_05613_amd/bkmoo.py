@@ -667,11 +667,14 @@ def adamw_table(params: Sequence[torch.Tensor], decay: Optional[Sequence[bool]] 
 def adamw(table: AdamwTable, grad: torch.Tensor, moment1: torch.Tensor, moment2: torch.Tensor, step: int,
           lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
           master: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
-          grad_scale: Optional[torch.Tensor] = None, seed: int = 0) -> None:
+          grad_scale: Optional[torch.Tensor] = None, seed: Optional[int] = None) -> None:
     """One AdamW step over the table's tensors, in place.  grad [N]: float32 or bfloat16, the tensors'
     gradients one after another (what resolve() returns).  moment1, moment2 [N]: float32, or
     float8_e4m3fn with scales float32 [2, blocks] (zeros to start with).  master: float32 [N] copy of
-    bfloat16 parameters that takes the step.  grad_scale: float32 tensor of one element."""
+    bfloat16 parameters that takes the step.  grad_scale: float32 tensor of one element.  seed: of the
+    random bits that round 8-bit moments, by default the step's number.  Every step needs another: with
+    the same bits again an element is rounded at the same place again, and moments that move by
+    less than the distance of two 8-bit values stay where they are."""
     dev, gpu, flat = table.device, table.device.index, (table.N,)
     f8 = moment1.dtype == torch.float8_e4m3fn
     sdt = torch.float8_e4m3fn if f8 else torch.float32
@@ -686,6 +689,6 @@ def adamw(table: AdamwTable, grad: torch.Tensor, moment1: torch.Tensor, moment2:
         if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev:
             raise ValueError(f"grad_scale must be one float32 value on {dev}")
         gs = grad_scale.data_ptr()
-    hp = _AdamwHparams(lr, beta1, beta2, eps, weight_decay, step, seed & 0xFFFFFFFF)
+    hp = _AdamwHparams(lr, beta1, beta2, eps, weight_decay, step, (step if seed is None else seed) & 0xFFFFFFFF)
     _run(_lib.bkmoo_adamw, "bkmoo_adamw", gpu, len(table.params), table.array, table.dt, table.N, gp, _dt(grad),
          STATE_F8 if f8 else STATE_F32, m1, m2, sc, table.blocks if f8 else 0, mp, ctypes.byref(hp), gs)
