@@ -20,6 +20,8 @@ namespace bkmoo {
 
 namespace {
 
+constexpr float kBf16Max = 0x1.fep127f;
+
 struct FewArgs {
   const void *x, *w0, *w1;     // [M][K]; [N][K] (w1: the up product's)
   void *out, *u, *v;           // [M][N]; u, v: may be null
@@ -31,7 +33,9 @@ struct FewArgs {
 // h is what the two kernels pass on.  Up to eight tokens of bf16 pass it on as two bf16, the second
 // what rounding leaves out of the first (2^-17 of it is lost then): a token's errors come from a
 // few large elements of h and do not average out.  The second product takes both as the 16 tokens
-// of a tile (SPLIT), at no cost.
+// of a tile (SPLIT), at no cost.  Where the first part's sum is not finite (an infinite weight, an
+// infinity or NaN in h) it is the result: the second part's may be an infinity of the other
+// sign, or NaN.
 
 // The waves' sums, added in wave order, and what becomes of them.
 template <typename T, bool PAIR, int R, int NT, int WAVES, bool SPLIT>
@@ -47,9 +51,14 @@ __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PA
       s[i] = sums[0][i * R + c][t][lane];
 #pragma unroll
       for (int q = 1; q < WAVES; ++q) s[i] += sums[q][i * R + c][t][lane];
-      if constexpr (SPLIT)
+      if constexpr (SPLIT) {
+        f32x4 both = s[i];
 #pragma unroll
-        for (int q = 0; q < WAVES; ++q) s[i] += sums[q][i * R + c][t][lane ^ 8];  // (token r + 8)
+        for (int q = 0; q < WAVES; ++q) both += sums[q][i * R + c][t][lane ^ 8];  // (token r + 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (__builtin_isfinite(s[i][e])) s[i][e] = both[e];
+      }
     }
     const int64_t m = t * 16 + r, n = n0 + c * 16 + 4 * g;
     if (m >= a.M) continue;
@@ -59,8 +68,14 @@ __device__ __forceinline__ void finish(const FewArgs &a, const f32x4 (*sums)[(PA
       if (n + e < a.N) {
         if constexpr (PAIR) {
           const float h = gate_act<T>(s[0][e], a.act) * s[1][e];
-          ((T *)a.out)[at + e] = (T)h;
-          if (a.lo) ((T *)a.lo)[at + e] = (T)(__builtin_isfinite(h) ? h - (float)(T)h : 0.0f);
+          T hi = (T)h;
+          if (a.lo) {
+            // (a finite h that rounds to infinity: the largest bf16, the rest in the second)
+            const bool fine = __builtin_isfinite(h);
+            if (fine && !__builtin_isfinite((float)hi)) hi = (T)copysignf(kBf16Max, h);
+            ((T *)a.lo)[at + e] = (T)(fine ? h - (float)hi : 0.0f);
+          }
+          ((T *)a.out)[at + e] = hi;
           if (a.u) {
             ((T *)a.u)[at + e] = (T)s[0][e];
             ((T *)a.v)[at + e] = (T)s[1][e];
