@@ -489,7 +489,7 @@ typedef struct {
 
 /* Hyper-parameters of an AdamW step (host struct). */
 typedef struct {
-  double lr, beta1, beta2, eps, weight_decay; /* lr, wd >= 0; betas in [0, 1); eps > 0 (also in fp32) */
+  double lr, beta1, beta2, eps, weight_decay; /* lr, wd >= 0; betas in [0, 1); eps >= 2^-126 (normal in fp32) */
   int64_t step;                               /* t >= 1: the first step is 1 */
   uint32_t seed;                              /* random bits of BKMOO_STATE_F8: another for every step */
 } bkmoo_adamw_hparams;

@@ -248,7 +248,8 @@ __device__ __forceinline__ void step8(const AdamArgs &a, T *p, const G *grad, fl
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[e] = sqrtf(q[e]);
   }
-  // (the reciprocal instruction is within an ulp; the step it scales is added to the parameter)
+  // (the reciprocal instruction is within an ulp, of a normal number, which eps sees to; the step it
+  // scales is added to the parameter)
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = x[e] * keep - a.step * m[e] * __builtin_amdgcn_rcpf(q[e] * a.rootc + a.eps);
   if (ALL || i < n) {
@@ -323,8 +324,9 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
   if (master && dt != BKMOO_BF16) return BKMOO_EINVAL;
   if (!(hp->lr >= 0.0) || !__builtin_isfinite(hp->lr) || !(hp->beta1 >= 0.0 && hp->beta1 < 1.0) ||
       !(hp->beta2 >= 0.0 && hp->beta2 < 1.0) || !(hp->eps > 0.0) || !__builtin_isfinite(hp->eps) ||
-      !(hp->weight_decay >= 0.0) || !__builtin_isfinite(hp->weight_decay) || hp->step < 1 || !((float)hp->eps > 0.0f))
+      !(hp->weight_decay >= 0.0) || !__builtin_isfinite(hp->weight_decay) || hp->step < 1)
     return BKMOO_EINVAL;
+  if ((float)hp->eps < __FLT_MIN__) return BKMOO_EINVAL;  // the reciprocal instruction takes such a number for zero
   const bool s8 = state_dt == BKMOO_STATE_F8;
   int64_t total = 0, blks = 0;
   for (int t = 0; t < T; ++t) {
