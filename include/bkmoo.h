@@ -584,7 +584,8 @@ bkmoo_status bkmoo_adamw_blocks(int32_t T, const bkmoo_tensor *tensors, int64_t 
  *   g = grad_scale * grad, m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
  *
- *   tensors    (host array) the parameters, of type dt; the decay term applies where decay is set
+ *   tensors    (host array) the parameters, of type dt, none over another (BKMOO_EINVAL: a weight
+ *              that two layers share is listed once); the decay term applies where decay is set
  *   grad       (in)  N = sum of n elements of grad_dt: the tensors' gradients one after another, as
  *              bkmoo_resolve leaves them
  *   moment1, moment2 (in/out) N elements in the same order.  BKMOO_STATE_F32: m and v, fp32.

@@ -30,6 +30,8 @@
 // rounded to the other e4m3 value, so the expressions up to there round as written.
 #include <math.h>
 
+#include <algorithm>
+
 #include "elem.h"
 #include "layer_common.h"
 
@@ -309,6 +311,48 @@ hipError_t launch(const AdamArgs &a, int64_t chunks, bool s8, bool fine, hipStre
 
 int64_t blocks_of(int64_t n) { return (n + kBlock - 1) / kBlock; }
 
+// Two of the tensors share a byte (they would be stepped by two workgroups at once).  Tensors in
+// ascending order, as one buffer's views are, need one look each.  Else kSorted of them at a time are
+// sorted, on the stack, and compared with each other and with all that come behind them: without an
+// allocation, which could fail here.
+bool tensors_overlap(int32_t T, const bkmoo_tensor *tensors, size_t es) {
+  constexpr int kSorted = 1024;
+  struct Span {
+    uintptr_t lo, hi;
+  };
+  auto span = [&](int32_t t) {
+    const uintptr_t p = (uintptr_t)tensors[t].data;
+    return Span{p, p + (size_t)tensors[t].n * es};
+  };
+  uintptr_t end = 0;
+  int32_t first = 0;
+  for (; first < T; ++first) {
+    if (tensors[first].n == 0) continue;
+    const Span x = span(first);
+    if (x.lo < end) break;
+    end = x.hi;
+  }
+  if (first == T) return false;
+  Span s[kSorted];
+  for (int32_t t = 0; t < T;) {
+    int n = 0;
+    for (; t < T && n < kSorted; ++t)
+      if (tensors[t].n > 0) s[n++] = span(t);
+    if (n == 0) return false;
+    std::sort(s, s + n, [](const Span &a, const Span &b) { return a.lo < b.lo; });
+    for (int i = 1; i < n; ++i)
+      if (s[i].lo < s[i - 1].hi) return true;
+    for (int32_t q = t; q < T; ++q) {
+      if (tensors[q].n == 0) continue;
+      const Span x = span(q);
+      // the first that starts behind x's start, and the one before it
+      const int i = (int)(std::upper_bound(s, s + n, x.lo, [](uintptr_t p, const Span &a) { return p < a.lo; }) - s);
+      if ((i < n && s[i].lo < x.hi) || (i > 0 && x.lo < s[i - 1].hi)) return true;
+    }
+  }
+  return false;
+}
+
 }  // namespace
 
 }  // namespace bkmoo
@@ -350,6 +394,7 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
     const Range p[] = {{tensors[t].data, (size_t)tensors[t].n * elem_bytes(dt)}};
     if (any_overlap(p, out) || any_overlap(in, p)) return BKMOO_EINVAL;
   }
+  if (tensors_overlap(T, tensors, elem_bytes(dt))) return BKMOO_EINVAL;
   AdamArgs a;
   a.grad = grad;
   a.m = moment1;

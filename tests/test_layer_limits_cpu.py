@@ -2,6 +2,7 @@
 pointers below are never dereferenced)."""
 
 import ctypes
+import random
 
 import pytest
 
@@ -32,3 +33,37 @@ def adamw(b, places, eps=1e-8, dt=0):
 def test_eps_below_the_normal_numbers(b, eps):
     """The step's reciprocal takes a denormal number for zero."""
     assert adamw(b, [(0, 64)], eps=eps) == EINVAL
+
+
+def apart(sizes, gap=0, es=4):
+    """Places of tensors one after another, `gap` bytes apart."""
+    out, p = [], 0
+    for n in sizes:
+        out.append((p, n))
+        p += n * es + gap
+    return out
+
+
+def test_tensors_over_one_another(b):
+    """Two tensors that share an element would be stepped at once: refused, in whatever order they come and
+    however many there are; neighbours are not."""
+    gen = random.Random(5)
+    for many in (2, 3, 50, 1024, 1025, 3000):
+        sizes = [gen.choice([0, 1, 2, 300]) for _ in range(many - 2)]
+        far = sum(sizes) * 4 + 4096
+        for first, second in (((far, 64), (far, 64)),             # one tensor twice
+                              ((far, 64), (far + 63 * 4, 5)),     # its last element
+                              ((far, 64), (far + 8, 1)),          # one within another
+                              ((far + 40, 64), (far, 11))):
+            for where in ("as they come", "behind", "mixed"):
+                places = apart(sizes)
+                places = [first] + places + [second] if where == "as they come" else places + [first, second]
+                if where == "mixed":
+                    gen.shuffle(places)
+                assert adamw(b, places) == EINVAL, (many, first, second, where)
+
+
+def test_empty_tensors_lie_over_nothing(b):
+    t = (b._Tensor * 3)((at(0), 0, 1), (at(0), 0, 1), (0, 0, 1))
+    hp = b._AdamwHparams(0.1, 0.9, 0.99, 1e-8, 0.0, 1, 0)
+    assert b._lib.bkmoo_adamw(3, t, 0, 0, None, 0, 0, None, None, None, 0, None, ctypes.byref(hp), None, None) == 0
