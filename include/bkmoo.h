@@ -508,14 +508,15 @@ typedef struct {
  *   post_weight, gate      (in)  [D] or NULL: no norm after the block, no gate
  *   resid_out, normed      (out) [M][D]; resid_out may be resid
  *
- * BKMOO_EUNSUPPORTED for rows of more than 64 KiB.
+ * BKMOO_EUNSUPPORTED for rows of more than 64 KiB and for M >= 2^31.
  */
 bkmoo_status bkmoo_residual_norm_forward(int64_t M, int64_t D, bkmoo_dtype dt, const void *resid, const void *y,
                                          const void *weight, const void *post_weight, const void *gate,
                                          double scale, double eps, void *resid_out, void *normed,
                                          hipStream_t stream);
 
-/* Workspace of bkmoo_residual_norm_backward (*bytes, host). */
+/* Workspace of bkmoo_residual_norm_backward (*bytes, host).  BKMOO_EUNSUPPORTED for K > 16, M >= 2^31
+ * or D > 32768 (64 KiB of bf16). */
 bkmoo_status bkmoo_residual_norm_workspace_size(int64_t M, int64_t D, int32_t K, size_t *bytes);
 
 /*
@@ -552,7 +553,7 @@ bkmoo_status bkmoo_ffn_workspace_size(int64_t M, int64_t D, int64_t F, bkmoo_dty
  *                                                   for the backward pass
  *
  * For more than eight rows h is rounded to dt between the products.
- * BKMOO_EUNSUPPORTED for D or F above 2^20.
+ * BKMOO_EUNSUPPORTED for D or F above 2^20 and for M >= 2^31.
  */
 bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, bkmoo_act act, const void *x,
                                const void *w_gate, const void *w_up, const void *w_down, void *y, void *gate_out,
@@ -575,7 +576,8 @@ bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt,
                                 void *dx, void *dw_gate, void *dw_up, void *dw_down, int64_t task_stride,
                                 void *workspace, size_t ws_bytes, hipStream_t stream);
 
-/* Blocks of 256 elements (the last of a tensor may be shorter) of T tensors (*blocks, host). */
+/* Blocks of 256 elements (the last of a tensor may be shorter) of T tensors (*blocks, host).
+ * BKMOO_EUNSUPPORTED for a tensor of more than 2^36 - 4096 elements, here and below. */
 bkmoo_status bkmoo_adamw_blocks(int32_t T, const bkmoo_tensor *tensors, int64_t *blocks);
 
 /*

@@ -44,6 +44,8 @@ constexpr int kChunk = 4096;            // elements of a workgroup
 constexpr int kAdamThreads = 256;
 constexpr int kLaneElems = 8;
 constexpr int kMaxTensors = 192;
+constexpr int64_t kMaxChunks = (1 << 24) - 1;  // a launch has fewer than 2^32 threads
+constexpr int64_t kMaxElems = kMaxChunks * kChunk, kMaxTotal = (int64_t)1 << 48;  // of a tensor, of all
 constexpr double kFineBeta = 0.98;
 constexpr float kF8Max = 448.0f;
 constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: a block below it holds zeros
@@ -376,10 +378,12 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
   for (int t = 0; t < T; ++t) {
     const int64_t n = tensors[t].n;
     if (n < 0 || n > N - total || (n > 0 && !tensors[t].data) || !natural(tensors[t].data, dt)) return BKMOO_EINVAL;
+    if (n > kMaxElems) return BKMOO_EUNSUPPORTED;
     total += n;
     blks += blocks_of(n);
   }
   if (total != N) return BKMOO_EINVAL;
+  if (N > kMaxTotal) return BKMOO_EUNSUPPORTED;
   if (s8 ? blocks != blks || (N > 0 && !scales) : scales != nullptr) return BKMOO_EINVAL;
   if (N > 0 && (!grad || !moment1 || !moment2)) return BKMOO_EINVAL;
   if (!natural(grad, grad_dt) || (uintptr_t)master % 4 || (uintptr_t)scales % 4 || (uintptr_t)grad_scale % 4 ||
@@ -422,8 +426,7 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
     for (; t < T && a.n < kMaxTensors; ++t) {
       const int64_t n = tensors[t].n, c = (n + kChunk - 1) / kChunk;
       if (n == 0) continue;
-      if (c > 0x7fffffff) return BKMOO_EUNSUPPORTED;
-      if (a.n > 0 && (chunks + c > 0x7fffffff || at + n - a.start0 > 0xffffffffll)) break;
+      if (a.n > 0 && (chunks + c > kMaxChunks || at + n - a.start0 > 0xffffffffll)) break;
       a.p[a.n] = tensors[t].data;
       a.start[a.n] = (uint32_t)(at - a.start0);
       a.block[a.n] = (uint32_t)(blk - a.block0);
@@ -450,6 +453,7 @@ extern "C" bkmoo_status bkmoo_adamw_blocks(int32_t T, const bkmoo_tensor *tensor
   int64_t n = 0;
   for (int t = 0; t < T; ++t) {
     if (tensors[t].n < 0) return BKMOO_EINVAL;
+    if (tensors[t].n > kMaxElems) return BKMOO_EUNSUPPORTED;
     n += blocks_of(tensors[t].n);
   }
   *blocks = n;

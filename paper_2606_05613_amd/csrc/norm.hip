@@ -400,6 +400,7 @@ __global__ __launch_bounds__(kSumCols *kSumGroups) void norm_sum_kernel(const No
 }
 
 constexpr int64_t kMaxRowBytes = 64 << 10;  // sixteen waves of four vectors
+constexpr int64_t kMaxRows = 0x7fffffff;
 // Workgroups of the backward pass, about one of 512 threads a CU (bf16's registers leave no room
 // for a second): a few more would take as long as all the others, and each writes sums of its
 // own.  Of rows of 300 bf16 three of 256 threads instead take 73 us, these 59.
@@ -462,7 +463,7 @@ hipError_t backward(const NormArgs &a, const NormSumArgs &sum, int chunks, hipSt
 bkmoo_status check_norm(int64_t M, int64_t D, int dt, double scale, double eps) {
   if (M < 0 || D < 1 || !valid_elem(dt) || !(eps >= 0.0) || !__builtin_isfinite(eps) || !__builtin_isfinite(scale))
     return BKMOO_EINVAL;
-  if (D * elem_bytes(dt) > kMaxRowBytes || M > 0x7fffffff) return BKMOO_EUNSUPPORTED;
+  if (D > kMaxRowBytes / elem_bytes(dt) || M > kMaxRows) return BKMOO_EUNSUPPORTED;
   return BKMOO_OK;
 }
 
@@ -505,7 +506,7 @@ extern "C" bkmoo_status bkmoo_residual_norm_forward(int64_t M, int64_t D, bkmoo_
 
 extern "C" bkmoo_status bkmoo_residual_norm_workspace_size(int64_t M, int64_t D, int32_t K, size_t *bytes) {
   if (M < 0 || D < 1 || K < 1 || !bytes) return BKMOO_EINVAL;
-  if (K > kMaxK) return BKMOO_EUNSUPPORTED;
+  if (K > kMaxK || M > kMaxRows || D > kMaxRowBytes / elem_bytes(BF16)) return BKMOO_EUNSUPPORTED;
   const int rows = chunk_rows_for(M, K);
   *bytes = align256((size_t)((M + rows - 1) / rows + K) * 2 * (size_t)D * sizeof(float));
   return BKMOO_OK;

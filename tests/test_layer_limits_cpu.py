@@ -7,7 +7,7 @@ import random
 import pytest
 
 FAKE = 0x7F0000000000
-EINVAL = -1
+EINVAL, EUNSUPPORTED = -1, -2
 
 
 @pytest.fixture(scope="module")
@@ -67,3 +67,28 @@ def test_empty_tensors_lie_over_nothing(b):
     t = (b._Tensor * 3)((at(0), 0, 1), (at(0), 0, 1), (0, 0, 1))
     hp = b._AdamwHparams(0.1, 0.9, 0.99, 1e-8, 0.0, 1, 0)
     assert b._lib.bkmoo_adamw(3, t, 0, 0, None, 0, 0, None, None, None, 0, None, ctypes.byref(hp), None, None) == 0
+
+
+def test_norm_sizes_past_the_limits(b):
+    """More rows or columns than the norms take, up to the ends of int64: refused by the size query too."""
+    L, size = b._lib, ctypes.c_size_t(0)
+    for M, D in ((255 << 32, 64), (1 << 31, 64), ((1 << 63) - 1, 64), (4, 32769), (4, 1 << 61), (4, (1 << 63) - 1)):
+        assert L.bkmoo_residual_norm_workspace_size(M, D, 1, ctypes.byref(size)) == EUNSUPPORTED, (M, D)
+    assert L.bkmoo_residual_norm_workspace_size((1 << 31) - 1, 32768, 16, ctypes.byref(size)) == 0
+    assert size.value <= (256 + 16) * 2 * 32768 * 4 + 256
+    for dt, D in ((0, 1 << 61), (0, 1 << 62), (1, 1 << 62), (1, (1 << 63) - 1), (0, (1 << 63) - 1)):
+        assert L.bkmoo_residual_norm_forward(0, D, dt, at(0), at(1), at(2), None, None, 1.0, 1e-6, at(3), at(4),
+                                             None) == EUNSUPPORTED, D
+
+
+def test_adamw_sizes_past_the_limits(b):
+    """Elements whose blocks of 256 or bytes would overflow 64 bits are refused, in the count of blocks too."""
+    blocks = ctypes.c_int64(0)
+    for n in ((1 << 63) - 1, (1 << 63) - 255, 1 << 48):
+        t = (b._Tensor * 1)((at(0), n, 1))
+        assert b._lib.bkmoo_adamw_blocks(1, t, ctypes.byref(blocks)) == EUNSUPPORTED, n
+        hp = b._AdamwHparams(0.1, 0.9, 0.99, 1e-8, 0.0, 1, 0)
+        assert b._lib.bkmoo_adamw(1, t, 0, n, at(1), 0, 0, at(2), at(3), None, 0, None, ctypes.byref(hp), None,
+                                  None) == EUNSUPPORTED, n
+    t = (b._Tensor * 1)((at(0), 1 << 35, 1))
+    assert b._lib.bkmoo_adamw_blocks(1, t, ctypes.byref(blocks)) == 0 and blocks.value == 1 << 27
