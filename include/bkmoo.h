@@ -490,6 +490,7 @@ typedef struct {
 /* Hyper-parameters of an AdamW step (host struct). */
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay; /* lr, wd >= 0; betas in [0, 1); eps >= 2^-126 (normal in fp32) */
+                                              /* 1 - lr wd and lr / (1 - beta1^t) finite in fp32 */
   int64_t step;                               /* t >= 1: the first step is 1 */
   uint32_t seed;                              /* random bits of BKMOO_STATE_F8: another for every step */
 } bkmoo_adamw_hparams;
@@ -508,6 +509,7 @@ typedef struct {
  *   post_weight, gate      (in)  [D] or NULL: no norm after the block, no gate
  *   resid_out, normed      (out) [M][D]; resid_out may be resid
  *
+ * scale and eps (>= 0) are finite in fp32, and an eps above zero is above it there.
  * BKMOO_EUNSUPPORTED for rows of more than 64 KiB and for M >= 2^31.
  */
 bkmoo_status bkmoo_residual_norm_forward(int64_t M, int64_t D, bkmoo_dtype dt, const void *resid, const void *y,

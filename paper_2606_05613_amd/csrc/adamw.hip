@@ -415,6 +415,7 @@ extern "C" bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmo
   a.step = (float)(hp->lr / (1.0 - pow(hp->beta1, (double)hp->step)));
   a.rootc = (float)(1.0 / sqrt(1.0 - pow(hp->beta2, (double)hp->step)));
   a.eps = (float)hp->eps;
+  if (!__builtin_isfinite(a.keep) || !__builtin_isfinite(a.step) || !__builtin_isfinite(a.eps)) return BKMOO_EINVAL;
   a.seed = hp->seed;
   const bool fine = hp->beta1 > kFineBeta || hp->beta2 > kFineBeta;
   int64_t at = 0, blk = 0;

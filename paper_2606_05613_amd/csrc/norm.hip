@@ -461,7 +461,9 @@ hipError_t backward(const NormArgs &a, const NormSumArgs &sum, int chunks, hipSt
 }
 
 bkmoo_status check_norm(int64_t M, int64_t D, int dt, double scale, double eps) {
-  if (M < 0 || D < 1 || !valid_elem(dt) || !(eps >= 0.0) || !__builtin_isfinite(eps) || !__builtin_isfinite(scale))
+  // (in the kernels' 32 bits: eps may be zero, but not become it)
+  if (M < 0 || D < 1 || !valid_elem(dt) || !(eps >= 0.0) || !__builtin_isfinite((float)eps) ||
+      (eps > 0.0 && (float)eps == 0.0f) || !__builtin_isfinite((float)scale))
     return BKMOO_EINVAL;
   if (D > kMaxRowBytes / elem_bytes(dt) || M > kMaxRows) return BKMOO_EUNSUPPORTED;
   return BKMOO_OK;

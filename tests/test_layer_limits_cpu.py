@@ -92,3 +92,21 @@ def test_adamw_sizes_past_the_limits(b):
                                   None) == EUNSUPPORTED, n
     t = (b._Tensor * 1)((at(0), 1 << 35, 1))
     assert b._lib.bkmoo_adamw_blocks(1, t, ctypes.byref(blocks)) == 0 and blocks.value == 1 << 27
+
+
+@pytest.mark.parametrize("scale,eps", [(1e39, 1e-6), (-1e300, 1e-6), (1.0, 1e39), (1.0, 1e-46)])
+def test_norm_scalars_that_fp32_cannot_hold(b, scale, eps):
+    """Finite in 64 bits, infinite (or zero, where it was not) in the kernels' 32."""
+    assert b._lib.bkmoo_residual_norm_forward(0, 64, 0, at(0), at(1), at(2), None, None, scale, eps, at(3), at(4),
+                                              None) == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(lr=1e39), dict(lr=1e20, wd=1e20), dict(lr=1e30, b1=1 - 1e-12)])
+def test_adamw_scalars_that_fp32_cannot_hold(b, bad):
+    """The rate, its product with the decay, or the rate over 1 - beta1^t."""
+    v = dict(lr=0.1, b1=0.9, wd=0.0)
+    v.update(bad)
+    t = (b._Tensor * 1)((at(0), 64, 1))
+    hp = b._AdamwHparams(v["lr"], v["b1"], 0.99, 1e-8, v["wd"], 1, 0)
+    assert b._lib.bkmoo_adamw(1, t, 0, 64, at(1), 0, 0, at(2), at(3), None, 0, None, ctypes.byref(hp), None,
+                              None) == EINVAL
