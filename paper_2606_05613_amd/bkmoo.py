@@ -636,12 +636,19 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate_out: torch.Tensor, up_o
     return dx
 
 
+_data_ptr = torch.Tensor.data_ptr
+
+
 class AdamwTable:
     """The addresses and sizes of adamw()'s tensors, in the order of the flat gradient.
-    N: their elements; blocks: their blocks of 256 elements (the scales of 8-bit moments)."""
+    N: their elements; blocks: their blocks of 256 elements (the scales of 8-bit moments).
+    A table keeps the tensors' memory.  Where one is given other memory afterwards (p.data = ...,
+    module.to(dtype), a storage's resize) adamw() refuses the table: lay out another."""
 
     def __init__(self, params: Sequence[torch.Tensor], decay: Optional[Sequence[bool]] = None):
-        self.params = list(params)  # keeps their memory
+        self.params = list(params)
+        self.memory = [p.detach() for p in self.params]  # a tensor alone does not keep the memory it has now
+        self.addresses = list(map(_data_ptr, self.params))
         if not self.params:
             raise ValueError("no tensors")
         self.dt, self.device = _dt(self.params[0]), _gpu(self.params[0], "parameters")
@@ -651,8 +658,8 @@ class AdamwTable:
         decay = [True] * len(self.params) if decay is None else list(decay)
         if len(decay) != len(self.params):
             raise ValueError("decay holds one entry for each tensor")
-        self.array = (_Tensor * len(self.params))(*[(p.data_ptr(), p.numel(), int(bool(d)))
-                                                    for p, d in zip(self.params, decay)])
+        self.array = (_Tensor * len(self.params))(*[(a, p.numel(), int(bool(d)))
+                                                    for a, p, d in zip(self.addresses, self.params, decay)])
         self.N = sum(p.numel() for p in self.params)
         n = ctypes.c_int64(0)
         _check(_lib.bkmoo_adamw_blocks(len(self.params), self.array, ctypes.byref(n)), "bkmoo_adamw_blocks")
@@ -676,6 +683,9 @@ def adamw(table: AdamwTable, grad: torch.Tensor, moment1: torch.Tensor, moment2:
     the same bits again an element is rounded at the same place again, and moments that move by
     less than the distance of two 8-bit values stay where they are."""
     dev, gpu, flat = table.device, table.device.index, (table.N,)
+    # (as the table keeps the old memory, no other can have its address)
+    if list(map(_data_ptr, table.params)) != table.addresses:
+        raise ValueError("a parameter's memory is not where it was: lay it out again with adamw_table()")
     f8 = moment1.dtype == torch.float8_e4m3fn
     sdt = torch.float8_e4m3fn if f8 else torch.float32
     gp = _ptr(grad, flat, grad.dtype, gpu, "grad")
