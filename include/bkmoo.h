@@ -602,9 +602,10 @@ bkmoo_status bkmoo_adamw_blocks(int32_t T, const bkmoo_tensor *tensors, int64_t 
  *
  * BKMOO_STATE_F8 rounds the moments stochastically, between the two e4m3 values around
  * each, with 8 random bits a moment (16 if a beta is above 0.98) mixed from `seed` and
- * the element's number; equal arguments give equal results.  A non-finite gradient makes its whole block's moments
- * non-finite.  The hyper-parameters are taken when the call is made (a captured graph
- * repeats them).
+ * the element's number; equal arguments give equal results.  A NaN among the gradients makes its own
+ * element's moments NaN and leaves its block's others as they are without it; an infinity makes the moments of its
+ * whole block non-finite (the block's scale is infinite), and with the next step its parameters.  The
+ * hyper-parameters are taken when the call is made (a captured graph repeats them).
  */
 bkmoo_status bkmoo_adamw(int32_t T, const bkmoo_tensor *tensors, bkmoo_dtype dt, int64_t N, const void *grad,
                          bkmoo_dtype grad_dt, bkmoo_state_dtype state_dt, void *moment1, void *moment2,

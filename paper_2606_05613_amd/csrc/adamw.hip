@@ -220,7 +220,9 @@ __device__ __forceinline__ void step8(const AdamArgs &a, T *p, const G *grad, fl
         wq[e + f] = fmaxf(round_f8(xq, rr[f]), xq > 0.0f ? 0.001953125f : 0.0f);
       }
     }
-    // a NaN or an infinity among them (or an overflow of the sum: nothing changes then)
+    // A NaN or an infinity among them (or an overflow of the sum: nothing changes then).  The maximum
+    // passes over a NaN: its own values are NaN, the block's others and its scale as without it.  An
+    // infinity is the maximum: the scale holds it, and zero times it is NaN for all.
     if (!(fabsf(odd) < __builtin_inff())) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
