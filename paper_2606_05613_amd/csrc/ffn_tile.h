@@ -448,7 +448,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
     nx.bstep = BKC ? 128 : BK * B.ld * ES;
     nx.left = (int)(x.K - k0);
     nx.t = t;
-    nx.seg_end = MODE == kInputGrad && seg == 0 ? x.steps_seg : x.t1;
+    // (a part of a split sum may end before its segment does)
+    nx.seg_end = MODE == kInputGrad && seg == 0 && x.steps_seg < x.t1 ? x.steps_seg : x.t1;
     nx.t1 = x.t1;
   };
   auto start_tile = [&](int round) {
