@@ -578,6 +578,17 @@ bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt,
                                 void *dx, void *dw_gate, void *dw_up, void *dw_down, int64_t task_stride,
                                 void *workspace, size_t ws_bytes, hipStream_t stream);
 
+/*
+ * bkmoo_set_ffn_tiles — force how the feed-forward block's products are cut: tiles of `side` x
+ * `side` (64, 128 or 256; 256 becomes 128 where an operand's rows are off four bytes), the sums
+ * of the down product, the hidden gradient and the input gradient in `splits` parts (1 to 16), at
+ * most `workgroups` workgroups (not for the hidden gradient).  0 restores the automatic choice of each.  Results depend on
+ * the sums' parts, by rounding, and on nothing else of it; sizes of workspaces change with it.
+ * Forward calls of up to 64 rows do not use these products.  Process-wide; for tests and tuning.
+ * BKMOO_EINVAL for any other value.
+ */
+bkmoo_status bkmoo_set_ffn_tiles(int32_t side, int32_t splits, int32_t workgroups);
+
 /* Blocks of 256 elements (the last of a tensor may be shorter) of T tensors (*blocks, host).
  * BKMOO_EUNSUPPORTED for a tensor of more than 2^36 - 4096 elements, here and below. */
 bkmoo_status bkmoo_adamw_blocks(int32_t T, const bkmoo_tensor *tensors, int64_t *blocks);

@@ -10,7 +10,7 @@ Names mirror include/bkmoo.h: workspace_size, gram, solve, combine, resolve,
 resolve_noalloc, conflicts, slice_offsets, gram_reduce, resolve_path, resolve_traffic,
 read_device_error, set_resolve_path, set_wait_limit, set_grid_override,
 status_string; and for the layer around the resolve residual_norm_forward,
-residual_norm_backward, ffn_forward, ffn_backward, adamw_table, adamw.
+residual_norm_backward, ffn_forward, ffn_backward, set_ffn_tiles, adamw_table, adamw.
 """
 
 from __future__ import annotations
@@ -88,6 +88,7 @@ def _load():
         "bkmoo_ffn_forward": [i64, i64, i64, cint, cint, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "bkmoo_ffn_backward": [i64, i64, i64, cint, cint, i32, i64p, vp, vp, vp, vp, vp, vp, vp,
                                vp, vp, vp, vp, i64, vp, sz, vp],
+        "bkmoo_set_ffn_tiles": [i32, i32, i32],
         "bkmoo_adamw_blocks": [i32, ctypes.POINTER(_Tensor), i64p],
         "bkmoo_adamw": [i32, ctypes.POINTER(_Tensor), cint, i64, vp, cint, cint, vp, vp, vp, i64, vp,
                         ctypes.POINTER(_AdamwHparams), vp, vp],
@@ -108,8 +109,8 @@ EXPORTS = ("bkmoo_workspace_size", "bkmoo_gram", "bkmoo_solve", "bkmoo_combine",
            "bkmoo_read_device_error", "bkmoo_set_grid_override", "bkmoo_resolve_path",
            "bkmoo_set_resolve_path", "bkmoo_set_wait_limit",
            "bkmoo_residual_norm_forward", "bkmoo_residual_norm_workspace_size", "bkmoo_residual_norm_backward",
-           "bkmoo_ffn_workspace_size", "bkmoo_ffn_forward", "bkmoo_ffn_backward", "bkmoo_adamw_blocks",
-           "bkmoo_adamw", "bkmoo_status_string")
+           "bkmoo_ffn_workspace_size", "bkmoo_ffn_forward", "bkmoo_ffn_backward",
+           "bkmoo_set_ffn_tiles", "bkmoo_adamw_blocks", "bkmoo_adamw", "bkmoo_status_string")
 
 
 def status_string(st: int) -> str:
@@ -634,6 +635,12 @@ def ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate_out: torch.Tensor, up_o
     _run(_lib.bkmoo_ffn_backward, "bkmoo_ffn_backward", gpu, M, D, F, code, ACTS[act], K, rows, *args, ws.data_ptr(),
          ws.numel())
     return dx
+
+
+def set_ffn_tiles(side: int = 0, splits: int = 0, workgroups: int = 0):
+    """Force the side (64, 128, 256) of the feed-forward products' tiles, the parts of their split sums and the
+    number of workgroups; 0: automatic (process-wide)."""
+    _check(_lib.bkmoo_set_ffn_tiles(int(side), int(splits), int(workgroups)), "bkmoo_set_ffn_tiles")
 
 
 _data_ptr = torch.Tensor.data_ptr

@@ -24,6 +24,7 @@ struct TileArgs {
   int64_t M, N, K;          // output rows and columns (kWeightGrad: of the first two matrices), length of the sum
   int64_t task_stride;      // elements from one task's gradient row to the next
   int tiles_m, tiles_n, problems, splits, act;
+  int workgroups;           // at most so many, but for the hidden gradient; 0: as many as the chip holds
   int64_t rows[kMaxK + 1];  // kWeightGrad: the tasks' rows
 };
 

@@ -1,5 +1,7 @@
 // The gated feed-forward block's entry points: argument checks, workspaces and
 // the choice of kernels.  The kernels are in ffn_tile.h.
+#include <atomic>
+
 #include "elem.h"
 #include "ffn.h"
 #include "layer_common.h"
@@ -18,6 +20,8 @@ constexpr int kMaxSplits = 16;
 struct Plan {
   int side, splits;
 };
+// bkmoo_set_ffn_tiles: 0 leaves the choice.
+std::atomic<int> g_side{0}, g_splits{0}, g_workgroups{0};
 
 // Estimated time of a product on `tiles` tiles of a CU, `steps` steps of 128 bytes along k each,
 // from times on MI355X.  bf16: a step of a tile of 256 takes a CU 1.8 us; of tiles of 128 one
@@ -56,6 +60,9 @@ Plan plan(int dt, Mode mode, int64_t M, int64_t N, int64_t K, int64_t problems, 
         best = Plan{side, splits};
       }
     }
+  const int side = g_side.load(), splits = g_splits.load();
+  if (side) best.side = side == 256 && !aligned ? 128 : side;
+  if (splits && mode != kGateUp && mode != kWeightGrad) best.splits = splits;
   return best;
 }
 
@@ -186,9 +193,12 @@ bkmoo_status check_ffn(int64_t M, int64_t D, int64_t F, int dt, int act) {
 }
 
 // A product of one matrix [M][N], the sum over K a segment (of kInputGrad's two) split where that fills the chip.
-hipError_t product(int dt, Mode mode, TileArgs g, int64_t M, int64_t N, int64_t K, float *partial, bool aligned,
-                   hipStream_t s) {
-  const Plan p = plan(dt, mode, M, N, mode == kInputGrad ? 2 * K : K, 1, aligned);
+// (`room` bytes for the parts: the workspace was laid out by the same plan, unless bkmoo_set_ffn_tiles came between.)
+hipError_t product(int dt, Mode mode, TileArgs g, int64_t M, int64_t N, int64_t K, float *partial, size_t room,
+                   bool aligned, hipStream_t s) {
+  Plan p = plan(dt, mode, M, N, mode == kInputGrad ? 2 * K : K, 1, aligned);
+  if ((size_t)p.splits * M * N * sizeof(float) > room) p.splits = 1;
+  g.workgroups = g_workgroups.load();
   g.M = M;
   g.N = N;
   g.K = K;
@@ -209,6 +219,15 @@ hipError_t launch_ffn_tile(int dt, Mode mode, const TileArgs &g, int tasks, bool
 }  // namespace bkmoo
 
 using namespace bkmoo;
+
+extern "C" bkmoo_status bkmoo_set_ffn_tiles(int32_t side, int32_t splits, int32_t workgroups) {
+  if ((side != 0 && side != 64 && side != 128 && side != 256) || splits < 0 || splits > kMaxSplits || workgroups < 0)
+    return BKMOO_EINVAL;
+  g_side.store(side);
+  g_splits.store(splits);
+  g_workgroups.store(workgroups);
+  return BKMOO_OK;
+}
 
 extern "C" bkmoo_status bkmoo_ffn_workspace_size(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, int32_t backward,
                                                  size_t *bytes) {
@@ -256,13 +275,14 @@ extern "C" bkmoo_status bkmoo_ffn_forward(int64_t M, int64_t D, int64_t F, bkmoo
   g.K = D;
   g.act = act == BKMOO_SILU ? kSilu : kGelu;
   g.splits = 1;
+  g.workgroups = g_workgroups.load();
   hipError_t e = launch_ffn_tile(dt, kGateUp, g, 1, aligned, plan(dt, kGateUp, M, 2 * F, D, 1, aligned).side, stream);
   if (e != hipSuccess) return BKMOO_EHIP;
   TileArgs d = {};
   d.a[0] = ws + L.h;
   d.b[0] = w_down;
   d.out[0] = y;
-  return status_of(product(dt, kDown, d, M, D, F, (float *)(ws + L.partial), aligned, stream));
+  return status_of(product(dt, kDown, d, M, D, F, (float *)(ws + L.partial), L.total - L.partial, aligned, stream));
 }
 
 extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmoo_dtype dt, bkmoo_act act, int32_t K,
@@ -303,7 +323,7 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
     g.out[1] = dv;
     g.out[2] = h;
     g.act = act == BKMOO_SILU ? kSilu : kGelu;
-    e = product(dt, kHiddenGrad, g, M, F, D, (float *)(ws + L.partial), aligned, stream);
+    e = product(dt, kHiddenGrad, g, M, F, D, (float *)(ws + L.partial), L.total - L.partial, aligned, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
     TileArgs d = {};
     d.a[0] = du;
@@ -311,7 +331,7 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
     d.b[0] = w_gate;
     d.b[1] = w_up;
     d.out[0] = dx;
-    e = product(dt, kInputGrad, d, M, D, F, (float *)(ws + L.partial), aligned, stream);
+    e = product(dt, kInputGrad, d, M, D, F, (float *)(ws + L.partial), L.total - L.partial, aligned, stream);
     if (e != hipSuccess) return BKMOO_EHIP;
   }
   TileArgs w = {};
@@ -328,6 +348,7 @@ extern "C" bkmoo_status bkmoo_ffn_backward(int64_t M, int64_t D, int64_t F, bkmo
   w.N = D;
   w.task_stride = task_stride;
   w.splits = 1;
+  w.workgroups = g_workgroups.load();
   for (int k = 0; k <= K; ++k) w.rows[k] = task_rows[k];
   return status_of(launch_ffn_tile(dt, kWeightGrad, w, K, aligned,
                                    plan(dt, kWeightGrad, F, D, (M + K - 1) / K, 3 * K, aligned).side, stream));

@@ -23,19 +23,23 @@ hipError_t launch_mode(TileArgs g, int tasks, int side, hipStream_t s) {
   // The hidden gradient's epilogue waits for loads of its own, which the next tile's would
   // hold up: a workgroup a tile (963 / 1079).
   const int64_t cus = MODE == kHiddenGrad ? n : device_cu_count();
+  auto workgroups = [&](int64_t most) {
+    if (MODE != kHiddenGrad && g.workgroups > 0) most = g.workgroups;
+    return (unsigned)(n < most ? n : most);
+  };
   if constexpr (ALIGNED) {
     if (side == 256) {
-      const unsigned grid = (unsigned)(n < cus ? n : cus);
+      const unsigned grid = workgroups(cus);
       ffn_tile_kernel<T, MODE, 256, 256, 2, 4, true><<<dim3(grid), dim3(512), 0, s>>>(g);
       return hipGetLastError();
     }
   }
   if (side == 64) {
-    const unsigned grid = (unsigned)(n < 4 * cus ? n : 4 * cus);
+    const unsigned grid = workgroups(4 * cus);
     ffn_tile_kernel<T, MODE, 64, 64, 4, 1, ALIGNED><<<dim3(grid), dim3(256), 0, s>>>(g);
     return hipGetLastError();
   }
-  const unsigned grid = (unsigned)(n < 2 * cus ? n : 2 * cus);
+  const unsigned grid = workgroups(2 * cus);
   ffn_tile_kernel<T, MODE, 128, 128, 2, 2, ALIGNED><<<dim3(grid), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
