@@ -289,6 +289,7 @@ constexpr int kDepth = [] {
 
 template <typename T, bool PAIR, int R, int NT, int WAVES, int KB, bool SPLIT = false>
 hipError_t launch_tiles(const FewArgs &a, hipStream_t s) {
+  static_assert(kDepth<PAIR, R, NT, WAVES, KB> >= 2, "a step travels while another is multiplied");
   ffn_few_kernel<T, PAIR, R, NT, WAVES, kDepth<PAIR, R, NT, WAVES, KB>, SPLIT>
       <<<dim3((unsigned)((a.N + 16 * R - 1) / (16 * R))), dim3(64 * WAVES), 0, s>>>(a);
   return hipGetLastError();
@@ -297,9 +298,15 @@ template <typename T, bool PAIR, int R, int WAVES, int KB>
 hipError_t launch(const FewArgs &a, hipStream_t s) {
   if constexpr (!PAIR && sizeof(T) == 2)
     if (a.lo) return launch_tiles<T, PAIR, R, 1, WAVES, KB, true>(a, s);
-  return a.M <= 16   ? launch_tiles<T, PAIR, R, 1, WAVES, KB>(a, s)
-         : a.M <= 32 ? launch_tiles<T, PAIR, R, 2, WAVES, KB>(a, s)
-                     : launch_tiles<T, PAIR, R, 4, WAVES, KB>(a, s);
+  // KB is what two workgroups a CU leave each.  Gate and up of 33 to 64 tokens in 16 columns a
+  // workgroup would have a ring of one step there, nothing on its way during the products: 96 give
+  // two, and these widths (below 4096) have at most one workgroup a CU (us, one step / two / three in
+  // 160 KB: 64 x 2048 x 4032 11.0 / 8.8 / 9.3, 64 x 1024 x 3584 6.5 / 6.0 / 6.4, 64 x 512 x 1408 4.6 / 4.9 / 5.1,
+  // fp32 64 x 1024 x 2048 16.1 / 13.6 / 14.0).  The result's ring has two as it is (four: 64 x 4096 x
+  // 14336 42.7 / 43.0).
+  if (a.M <= 16) return launch_tiles<T, PAIR, R, 1, WAVES, KB>(a, s);
+  if (a.M <= 32) return launch_tiles<T, PAIR, R, 2, WAVES, KB>(a, s);
+  return launch_tiles<T, PAIR, R, 4, WAVES, (PAIR && R == 1 ? 96 : KB)>(a, s);
 }
 
 template <typename T, bool PAIR, int NT, int U, bool SPLIT = false>
