@@ -12,6 +12,7 @@ enum Mode : int {
   kGateUp,      // u = x Wg^T, v = x Wu^T -> h = a(u) v (and u, v)
   kDown,        // y = h Wd^T
   kHiddenGrad,  // dh = dy Wd -> du = dh v a'(u), dv = dh a(u), h = a(u) v
+  kHiddenPart,  // a part of dh's sum
   kInputGrad,   // dx = du Wg + dv Wu
   kWeightGrad   // per task: dWg = du^T x, dWu = dv^T x, dWd = dy^T h
 };

@@ -263,15 +263,6 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
   } else if constexpr (MODE == kHiddenGrad) {
     const T *pu = (const T *)g.u, *pv = (const T *)g.v;
     T *du = (T *)g.out[0], *dv = (T *)g.out[1], *h = (T *)g.out[2];
-    if (g.splits > 1) {  // a part of dh's sum
-      float *part = g.partial + (int64_t)prob * Mo * No;
-      everywhere([&](auto all, int i, int q, int64_t at, int n) {
-        float x[8];
-        eight_columns(acc[i][2 * q], acc[i][2 * q + 1], x);
-        put(all, part + at, x, n);
-      });
-      return;
-    }
     auto finish = [&](auto all, int i, int q, int64_t at, int n, const float (&u)[8], const float (&v)[8]) {
       float d[8], xu[8], xv[8], xh[8];
       eight_columns(acc[i][2 * q], acc[i][2 * q + 1], d);
@@ -288,7 +279,9 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
       put(all, h + at, xh, n);
     };
     // u and v of the next row of pieces travel while this one is worked on (past an end: of the
-    // last row or zeros)
+    // last row or zeros; there tiles of 256 load them where they are used: the code for both ends
+    // left 21 registers in scratch memory, and 42 with a form for the parts of a split sum beside them, where this
+    // has 4: 8192 x 4096 x 14336 1031 us, 1011 and 997)
     Eight<T> nu[2][kPairs], nv[2][kPairs];
     auto ask = [&](auto all, int i) {
 #pragma unroll
@@ -322,8 +315,23 @@ __device__ __forceinline__ void store_tile(const TileArgs &g, const f32x4 (&acc)
     };
     if (inside)
       work(std::true_type{});
-    else
+    else if constexpr (BM < 256)
       work(std::false_type{});
+    else
+      each(std::false_type{}, [&](auto all, int i, int q, int64_t at, int n) {
+        float u[8], v[8];
+        const int64_t m = mrow + i * 16, row = (m < Mo ? m : Mo - 1) * No;
+        guarded_load8(pu + row, nwave + q * 32, No).get(u);
+        guarded_load8(pv + row, nwave + q * 32, No).get(v);
+        finish(all, i, q, at, n, u, v);
+      });
+  } else if constexpr (MODE == kHiddenPart) {
+    float *part = g.partial + (int64_t)prob * Mo * No;
+    everywhere([&](auto all, int i, int q, int64_t at, int n) {
+      float x[8];
+      eight_columns(acc[i][2 * q], acc[i][2 * q + 1], x);
+      put(all, part + at, x, n);
+    });
   } else {
     T *out = MODE == kWeightGrad ? (T *)g.out[prob % 3] + (prob / 3) * g.task_stride : (T *)g.out[0];
     float *part = nullptr;
@@ -368,7 +376,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(BKMOO_LDS unsigned char *)lds;
   const int tiles = g.tiles_m * g.tiles_n, total = tiles * g.problems;
-  constexpr bool kMany = MODE != kHiddenGrad;  // tiles a workgroup (at least one: the grid is no larger)
+  constexpr bool kMany = MODE != kHiddenGrad && MODE != kHiddenPart;  // tiles a workgroup (at least one: the grid is no larger)
 
   // A tile: its problem, its place, and its steps t0 to t1 (all, or its share of a
   // split sum).
@@ -403,7 +411,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void ffn_tile_kernel(const TileArg
     x.steps_seg = (int)((x.K + BK - 1) / BK);
     x.t0 = 0;
     x.t1 = x.steps_seg * (MODE == kInputGrad ? 2 : 1);
-    if constexpr (MODE == kDown || MODE == kHiddenGrad || MODE == kInputGrad) {
+    if constexpr (MODE == kDown || MODE == kHiddenPart || MODE == kInputGrad) {
       if (g.splits > 1) {
         const int per = (x.t1 + g.splits - 1) / g.splits;
         x.t0 = x.prob * per < x.t1 ? x.prob * per : x.t1;

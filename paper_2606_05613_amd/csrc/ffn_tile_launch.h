@@ -22,9 +22,10 @@ hipError_t launch_mode(TileArgs g, int tasks, int side, hipStream_t s) {
   // with loads and reads placed by rows of pieces).
   // The hidden gradient's epilogue waits for loads of its own, which the next tile's would
   // hold up: a workgroup a tile (963 / 1079).
-  const int64_t cus = MODE == kHiddenGrad ? n : device_cu_count();
+  constexpr bool one = MODE == kHiddenGrad || MODE == kHiddenPart;
+  const int64_t cus = one ? n : device_cu_count();
   auto workgroups = [&](int64_t most) {
-    if (MODE != kHiddenGrad && g.workgroups > 0) most = g.workgroups;
+    if (!one && g.workgroups > 0) most = g.workgroups;
     return (unsigned)(n < most ? n : most);
   };
   if constexpr (ALIGNED) {
@@ -54,6 +55,9 @@ hipError_t launch_ffn_tile_of(Mode mode, const TileArgs &g, int tasks, bool alig
     case kHiddenGrad:
       return aligned ? launch_mode<T, kHiddenGrad, true>(g, tasks, side, s)
                      : launch_mode<T, kHiddenGrad, false>(g, tasks, side, s);
+    case kHiddenPart:
+      return aligned ? launch_mode<T, kHiddenPart, true>(g, tasks, side, s)
+                     : launch_mode<T, kHiddenPart, false>(g, tasks, side, s);
     case kInputGrad:
       return aligned ? launch_mode<T, kInputGrad, true>(g, tasks, side, s)
                      : launch_mode<T, kInputGrad, false>(g, tasks, side, s);
