@@ -28,8 +28,9 @@ std::atomic<int> g_side{0}, g_splits{0}, g_workgroups{0};
 // 1.0 and two side by side 1.2, of 64 0.56 to 0.95 for one to four: small tiles lose to L2 and
 // LDS traffic, large ones to CUs without one.  fp32 is bound by the matrix cores at every
 // side.  The epilogue adds what its accesses take, the hidden gradient's the most (us at 128
-// and 256: 3000 x 1024 x 3000 51 and 51, 4096 x 2048 x 6144 157 and 165, 6000 x 512 x 1500 43 and 46, 2000 x
-// 1500 x 4500 76 and 67).  (us at 64 / 128 / 256,
+// and 256: 3000 x 1024 x 3000 51 and 51, 4096 x 2048 x 6144 157 and 165, 6000 x 512 x 1500 43 and 46, 1500 x 2048 x 6144
+// 84 and 90, 2000 x 1500 x 4500 76 and 68: priced so that the large side is taken from where it wins for
+// certain).  (us at 64 / 128 / 256,
 // M x D x F: gate and up 100 x 2048 x 6144 22 / 32 / 60, 1000 x 1024 x 3000 26 / 23 / 34, 512 x
 // 4096 x 14336 240 / 153 / 115; fp32 weight gradients 777 x 500 x 1364 42 / 46 / 82.)
 double product_us(int side, int dt, Mode mode, int64_t tiles, int64_t steps, bool aligned) {
@@ -42,7 +43,7 @@ double product_us(int side, int dt, Mode mode, int64_t tiles, int64_t steps, boo
     step = side == 256 ? 1.8 * t : side == 128 ? 1.2 * (t / 2) + 1.0 * (t % 2) : 0.95 * (t / 4) + four[t % 4];
   if (!aligned) step *= 1.5;
   const double end = mode != kHiddenGrad ? (side == 256 ? 8.0 : side == 128 ? 2.5 : 1.0)
-                                         : (side == 256 ? 26.0 : side == 128 ? 7.5 : 3.0);
+                                         : (side == 256 ? 36.0 : side == 128 ? 7.5 : 3.0);
   return steps * step + t * end;
 }
 
