@@ -11,6 +11,10 @@ resolve_noalloc, conflicts, slice_offsets, gram_reduce, resolve_path, resolve_tr
 read_device_error, set_resolve_path, set_wait_limit, set_grid_override,
 status_string; and for the layer around the resolve residual_norm_forward,
 residual_norm_backward, ffn_forward, ffn_backward, set_ffn_tiles, adamw_table, adamw.
+
+The calls take and fill tensors' memory and know nothing of autograd: outputs of inputs
+that require gradients have no graph, and tensors that a call writes (adamw()'s
+parameters among them) keep their autograd version.
 """
 
 from __future__ import annotations

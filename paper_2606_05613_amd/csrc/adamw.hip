@@ -19,12 +19,13 @@
 // step can be repeated.  Eight bits a moment, one mix for two elements, resolve a 512th of
 // the distance between values; a moment that a step moves by less would stay, so where
 // a beta is above kFineBeta (a step moves a moment by at most a fiftieth of what it differs
-// from its mean by) each element gets a mix of its own, sixteen bits a moment.  A root that is not zero stays so (the next step divides by
-// it).  The parameter takes the step from the unrounded moments.
+// from its mean by) each element gets a mix of its own, sixteen bits a moment.  A root that is not zero
+// stays so (the next step divides by it).  The parameter takes the step from the unrounded moments.
 //
 // Measured, 200 million elements: fp32 throughout 1067 us (5.2 TB/s), bf16 with fp32 copy and
-// moments 1043 (5.4), with 8-bit moments 601 (5.3), these without the copy 419 (4.8: the random
-// bits and the maxima are no longer hidden).  168 tensors of 2048: 4.7 us in one launch.
+// moments 1043 (5.4), with 8-bit moments 601-636 (5.0-5.3), these without the copy 419-445 (4.5-4.8: the random
+// bits and the maxima are no longer hidden).  Sixteen bits a moment (beta2 = 0.999) cost nothing
+// on top: 597 (5.4) and 439 (4.6).  168 tensors of 2048: 4.7 us in one launch.
 //
 // The unit is built without contraction: a moment one place off is now and then
 // rounded to the other e4m3 value, so the expressions up to there round as written.

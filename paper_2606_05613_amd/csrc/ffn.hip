@@ -12,7 +12,7 @@ namespace bkmoo {
 namespace {
 
 constexpr int64_t kMaxWidth = 1 << 20;
-constexpr int kCus = 256;        // MI355X
+constexpr int kCus = 256;        // MI355X (not the device's count: the workspace's size and the sums' order hang on the plan)
 constexpr int kMaxSplits = 16;
 
 // How a product is cut: tiles of side x side, the sum over k in `splits` parts (partial sums in
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float *part, int s
     if (i + e < n) out[i + e] = (T)s[e];
 }
 
-// The same for dh, and what the hidden gradient's epilogue makes of it.  (Few rows of a wide model: F / 64 tiles
+// The same for dh, and what the hidden gradient's epilogue makes of it, rounded to T as there.  (Few rows of a wide model: F / 64 tiles
 // alone do not fill the chip.  The product whole / in parts with this kernel, us: 16 x 2048 x 6144 bf16 22.5 /
 // 9.1 + 4.3, fp32 64 / 19.6 + 5.6; 16 x 4096 x 14336 bf16 61 / 37.5 + 4.3; 200 x 2048 x 6144 fp32 88 / 63 + 8.8.)
 template <typename T>

@@ -9,7 +9,8 @@
 //
 // us, gate and up / down: D=2048 F=6144, one token 9.9 / 7.8 (75 MB at 4.3 TB/s), 24 tokens
 // 10.4 / 8.4; D=4096 F=14336, one 41.9 / 21.7 (352 MB at 5.5 TB/s), 24 44.9 / 27.9, 64
-// 51.9 / 42.7.  Loads straight into the matrix layout instead of LDS, which ask for 16
+// 51.9 / 42.7.  fp32, both: D=2048 F=6144 1, 24 and 64 tokens 36.5, 48.0 and 79.0 (151 MB at 4.1 TB/s for one), D=4096
+// F=14336 133, 154 and 250 (5.3): at 64 the matrix cores, a tenth as fast as bf16's, take more than half of it.  Loads straight into the matrix layout instead of LDS, which ask for 16
 // bytes of 16 rows in turn, four times the look-ups of lines: 46.3 / 22.2 and, with 24 tokens, 58.7
 // / 36.7.
 #include "elem.h"
@@ -30,7 +31,8 @@ struct FewArgs {
   int act;
 };
 
-// h is what the two kernels pass on.  Up to eight tokens of bf16 pass it on as two bf16, the second
+// h is what the two kernels pass on, rounded to T: the operand type of the second product's matrix
+// instructions.  Up to eight tokens of bf16 pass it on as two bf16, the second
 // what rounding leaves out of the first (2^-17 of it is lost then): a token's errors come from a
 // few large elements of h and do not average out.  The second product takes both as the 16 tokens
 // of a tile (SPLIT), at no cost.  Where the first part's sum is not finite (an infinite weight, an

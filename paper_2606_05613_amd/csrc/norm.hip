@@ -9,7 +9,9 @@
 // Everything is a sum over a row or a column of M x D elements that are read
 // once: memory-bound.  A row stays in registers as it was read (16-byte vectors,
 // at any alignment) between its statistics and its results, so each input is
-// read once and each output written once; sums are fp32.  A workgroup goes
+// read once and each output written once; sums are fp32.  Backward passes over rows of more than 8192
+// elements read a row again, out of the caches, in each of its three phases, and in part hold the column sums in scratch
+// memory.  A workgroup goes
 // through rows with as many waves on a row as it has vectors of 64 lanes (and several
 // rows side by side where that is few), the next row's loads on their way.  The weight gradients'
 // column sums run over chunks of rows in fp32 registers (the p and g gradients
@@ -19,7 +21,10 @@
 // Measured, bf16 with both norms and the gate: 16384 x 4096 forward 102 us (537 MB at 5.3 TB/s),
 // backward 168 (806 MB at 4.8), 65536 x 1024 102 and 166; fp32 16384 x 4096 207 and 324.
 // One row of 4096 2.8 us, which is a kernel's start and end, and 4.8 + 3.4.  Narrow rows lose to their
-// reductions: 30000 x 300 19 (3.7 TB/s) and 63 (1.7).
+// reductions: 30000 x 300 19 (3.7 TB/s) and 63 (1.7).  Rows off 16 bytes lose a fifth forward and a third
+// backward (8192 x 8191 bf16 128 and 229, x 8192 95 and 153); long ones to registers: bf16 4096 x 16384 107 (5.0
+// TB/s) and 253 (3.2), x 16383 146 and 608, 2048 x 32768 252 (2.1) and 871 (0.9); fp32 4096 x 16384 194 (5.6) and
+// 1035 (1.6).
 #include "elem.h"
 #include "layer_common.h"
 
@@ -401,7 +406,8 @@ __global__ __launch_bounds__(kSumCols *kSumGroups) void norm_sum_kernel(const No
 
 constexpr int64_t kMaxRowBytes = 64 << 10;  // sixteen waves of four vectors
 constexpr int64_t kMaxRows = 0x7fffffff;
-// Workgroups of the backward pass, about one of 512 threads a CU (bf16's registers leave no room
+// Workgroups of the backward pass (not the device's count: the workspace's size and the sums' order
+// hang on it), about one of 512 threads a CU (bf16's registers leave no room
 // for a second): a few more would take as long as all the others, and each writes sums of its
 // own.  Of rows of 300 bf16 three of 256 threads instead take 73 us, these 59.
 constexpr int kTargetChunks = 256;
