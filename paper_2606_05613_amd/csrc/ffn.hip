@@ -12,7 +12,7 @@ namespace bkmoo {
 namespace {
 
 constexpr int64_t kMaxWidth = 1 << 20;
-constexpr int kCus = 256;        // MI355X (not the device's count: the workspace's size and the sums' order hang on the plan)
+constexpr int kCus = 256;  // MI355X (not the device's count: the workspace's size and the sums' order hang on the plan)
 constexpr int kMaxSplits = 16;
 
 // How a product is cut: tiles of side x side, the sum over k in `splits` parts (partial sums in
@@ -206,8 +206,8 @@ hipError_t product(int dt, Mode mode, TileArgs g, int64_t M, int64_t N, int64_t 
   g.K = K;
   g.splits = p.splits;
   g.partial = partial;
-  const Mode one = mode == kHiddenGrad && g.splits > 1 ? kHiddenPart : mode;
-  const hipError_t e = launch_ffn_tile(dt, one, g, 1, aligned, p.side, s);
+  const Mode kernel = mode == kHiddenGrad && g.splits > 1 ? kHiddenPart : mode;
+  const hipError_t e = launch_ffn_tile(dt, kernel, g, 1, aligned, p.side, s);
   if (e != hipSuccess || g.splits == 1) return e;
   return dt == F32 ? join<float>(mode, g, s) : join<__bf16>(mode, g, s);
 }

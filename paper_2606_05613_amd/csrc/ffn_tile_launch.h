@@ -22,10 +22,10 @@ hipError_t launch_mode(TileArgs g, int tasks, int side, hipStream_t s) {
   // with loads and reads placed by rows of pieces).
   // The hidden gradient's epilogue waits for loads of its own, which the next tile's would
   // hold up: a workgroup a tile (963 / 1079).
-  constexpr bool one = MODE == kHiddenGrad || MODE == kHiddenPart;
-  const int64_t cus = one ? n : device_cu_count();
+  constexpr bool tile_each = MODE == kHiddenGrad || MODE == kHiddenPart;
+  const int64_t cus = tile_each ? n : device_cu_count();
   auto workgroups = [&](int64_t most) {
-    if (!one && g.workgroups > 0) most = g.workgroups;
+    if (!tile_each && g.workgroups > 0) most = g.workgroups;
     return (unsigned)(n < most ? n : most);
   };
   if constexpr (ALIGNED) {
